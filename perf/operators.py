@@ -257,17 +257,17 @@ def prepare(case, seed):
         return s
     if case["kind"] == "reorder":
         k, v = _cache(case, g)
-        lens = torch.tensor(_lens(case), dtype=torch.int32)
         s["src"] = torch.tensor(_map(case), dtype=torch.int32, device="cuda")
         if own:
+            from paper_2403_18647_amd import binding as B
             s["ctx"] = _context(case["heads"], case["head_dim"], case["dtype"], case["layers"], case["batch"],
                                 case["slots"], 1)
             s["k"], s["v"], s["lens"] = s["ctx"].cache()
             s["k"].copy_(k)
             s["v"].copy_(v.view(s["v"].shape))
-            s["lens"].copy_(lens)
+            B.sdsat_set_cache_len(s["ctx"].handle, _lens(case))
         else:
-            s["k"], s["v"], s["lens"] = k, v, lens.cuda()
+            s["k"], s["v"], s["lens"] = k, v, torch.tensor(_lens(case), dtype=torch.int32, device="cuda")
         return s
     kp, vp, ko, vo, s["q"] = _shared(case, g)
     batch, q, pre, mine = case["groups"] * case["n"], case["q"], _prefixes(case), _owns(case)
