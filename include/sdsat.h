@@ -129,6 +129,25 @@ const int32_t* sdsat_cache_len_ptr(const sdsat_ctx* ctx);
 int sdsat_forward_block(sdsat_ctx* ctx, int32_t batch, int32_t q, const int32_t* d_tokens,
                         const uint64_t* d_ancestor_mask, float* d_logits);
 
+/* sdsat_forward_block for sequences that share a prefix (samples of one prompt,
+ * questions behind one instruction), which is then read once for all of them.
+ * The batch is cut into groups of `group` neighbouring sequences (batch must be
+ * a multiple of it, at most 64 groups).  The sequences of group i have the same
+ * first h_prefix_len[i] committed tokens (host array [batch / group]); their K
+ * and V lie in the cache of the group's first sequence.  A prefix is shared in
+ * whole 32-slot pages: of the other sequences, slots below
+ * 32 * (h_prefix_len[i] / 32) are not read, the rest of the prefix must be in
+ * each one's own slots (sdsat_kv_reorder with first_slot = the prefix length
+ * puts it there).  Every sequence's cache_len counts the prefix and must be at
+ * least as long (SDSAT_ECAPACITY, or SDSAT_EDATA later where only the device
+ * knows).  Outputs, masks and the tentative K and V as sdsat_forward_block; a
+ * row's attention is summed in another order than there, the same for every
+ * block of up to 64 rows per sequence.  group 1 is sdsat_forward_block.
+ * Stream-ordered; h_prefix_len is read during the call. */
+int sdsat_forward_block_shared(sdsat_ctx* ctx, int32_t batch, int32_t q, int32_t group,
+                               const int32_t* h_prefix_len, const int32_t* d_tokens,
+                               const uint64_t* d_ancestor_mask, float* d_logits);
+
 /* Greedy verification, Eq. 3.  d_tokens_out[b*q + j] = arg-max of logits row
  * (b, j) (lowest id among ties).  With d_drafts ([batch, q-1]: the tokens the
  * block fed at rows 1..q-1), d_n_accept[b] = the number m of leading j >= 1
@@ -154,6 +173,24 @@ int sdsat_verify_nucleus(sdsat_ctx* ctx, int32_t batch, int32_t q, const float* 
                          uint64_t seed, const int32_t* d_pos0, int32_t* d_tokens_out,
                          int32_t* d_n_accept);
 
+/* Log probabilities for ranking and reporting completions.  For each logits row
+ * (b, j) of [batch*q, V] float32, with z = logits / temperature (> 0, finite):
+ *   d_logprob[b*q + j]  log softmax(z)[d_tokens[b*q + j]]; 0 where the token is
+ *                       negative (a row without one); a token >= V gives NaN
+ *                       and SDSAT_EDATA at the next synchronous call;
+ *   d_entropy[b*q + j]  -sum p log p in nats (an id with logit -inf adds 0);
+ *   d_top_ids, d_top_logprobs [batch*q, n_top]  the n_top most probable ids and
+ *                       their log probabilities, the largest first, ties to the
+ *                       lower id (NaN logits last).
+ * n_top 0..32, at most V, V / 8192 * n_top <= 4096 (SDSAT_EUNSUPPORTED).
+ * d_logprob (with d_tokens), d_entropy and, with n_top 0, the last two may be
+ * NULL.  A row that holds NaN or whose largest logit is infinite (an empty row
+ * of -inf among them) gives NaN log probabilities and entropy.  float32
+ * arithmetic in a fixed order.  Stream-ordered. */
+int sdsat_token_logprobs(sdsat_ctx* ctx, int32_t batch, int32_t q, const float* d_logits,
+                         const int32_t* d_tokens, float temperature, int32_t n_top, float* d_logprob,
+                         float* d_entropy, int32_t* d_top_ids, float* d_top_logprobs);
+
 /* Commit block rows to the KV cache (the step after Eq. 1 keeps row 0, the
  * step after Eq. 3 keeps rows 0..m).  d_n_commit[b] rows of sequence b become
  * committed: cache_len[b] += n.  d_rows NULL: the committed rows are block rows
@@ -163,6 +200,26 @@ int sdsat_verify_nucleus(sdsat_ctx* ctx, int32_t batch, int32_t q, const float* 
  * case).  q is the row stride of d_rows.  Stream-ordered. */
 int sdsat_commit_kv(sdsat_ctx* ctx, int32_t batch, int32_t q, const int32_t* d_n_commit,
                     const int32_t* d_rows);
+
+/* Reorder the cache: sequence b < batch continues from sequence d_src[b], as its
+ * cache and cache_len stood before the call.  Any map: one prompt forked into
+ * samples (0, 0, 0, 0), beams that follow their parents, swaps and cycles, the
+ * survivors of a batch moved into the rows of finished sequences; d_src[b] = b
+ * stays, -1 frees sequence b (cache_len 0).  Sources may be any sequence below
+ * max_batch; one that is not (SDSAT_EDATA at the next synchronous call) leaves
+ * sequence b as it was.  Whole 32-slot pages move, in every layer, from the one
+ * that holds first_slot to the last with a committed slot of the source; the
+ * ones before are left as they are (a prefix that the sequences share or all
+ * hold).  Slots past cache_len are unspecified afterwards (a block's tentative
+ * rows do not move).  In place; needs max_batch <= 1024.  Stream-ordered. */
+int sdsat_kv_reorder(sdsat_ctx* ctx, int32_t batch, const int32_t* d_src, int32_t first_slot);
+
+/* Device pointers to one layer of the cache in the configuration's type, for
+ * saving pages and putting them back (in stream order; values must be finite):
+ * K [max_batch][n_heads][S][head_dim] and V [max_batch][n_heads][S/32][head_dim][32]
+ * with S = max_ctx rounded up to 32 and, within a page, the key 16a + 4g + r
+ * (a < 2, g < 4, r < 4) at place 8g + 4a + r. */
+int sdsat_cache_ptr(const sdsat_ctx* ctx, int32_t layer, void** d_k, void** d_v);
 
 /* Full SDSAT generation (Section 2.1): prefill of h_prompts[b][0..P-2]
  * (blocks of max_block rows, LM head skipped), then loops of draft step 1,
@@ -225,6 +282,14 @@ int sdsat_kv_write(sdsat_ctx* ctx, int32_t layer, int32_t batch, int32_t n, cons
  * sdsat_forward_block.  d_out: [batch*q, H*Dh] float32.  Stream-ordered. */
 int sdsat_attention(sdsat_ctx* ctx, int32_t layer, int32_t batch, int32_t q, const float* d_q,
                     const uint64_t* d_ancestor_mask, float* d_out);
+
+/* sdsat_attention for groups of sequences that share a prefix, as in
+ * sdsat_forward_block_shared (group, h_prefix_len and masks as there; d_q and
+ * d_out as in sdsat_attention).  A row whose mask leaves it no key gives zeros.
+ * Ancestor masks need q <= 64.  Stream-ordered. */
+int sdsat_attention_shared(sdsat_ctx* ctx, int32_t layer, int32_t batch, int32_t q, int32_t group,
+                           const int32_t* h_prefix_len, const float* d_q,
+                           const uint64_t* d_ancestor_mask, float* d_out);
 
 /* Bytes of the packed form of an [N, K] weight matrix. */
 size_t sdsat_linear_packed_bytes(int32_t dtype, int32_t N, int32_t K);

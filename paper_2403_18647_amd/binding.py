@@ -49,7 +49,11 @@ _SIGNATURES = {
     "sdsat_forward_block": ([_VP, _I32, _I32, _VP, _VP, _VP], _I32),
     "sdsat_verify_greedy": ([_VP, _I32, _I32, _VP, _VP, _VP, _VP], _I32),
     "sdsat_verify_nucleus": ([_VP, _I32, _I32, _VP, _VP, _F32, _F32, _I32, _U64, _VP, _VP, _VP], _I32),
+    "sdsat_forward_block_shared": ([_VP, _I32, _I32, _I32, ctypes.POINTER(_I32), _VP, _VP, _VP], _I32),
+    "sdsat_token_logprobs": ([_VP, _I32, _I32, _VP, _VP, _F32, _I32, _VP, _VP, _VP, _VP], _I32),
     "sdsat_commit_kv": ([_VP, _I32, _I32, _VP, _VP], _I32),
+    "sdsat_kv_reorder": ([_VP, _I32, _VP, _I32], _I32),
+    "sdsat_cache_ptr": ([_VP, _I32, ctypes.POINTER(_VP), ctypes.POINTER(_VP)], _I32),
     "sdsat_generate": ([_VP, _I32, ctypes.POINTER(_I32), _I32, _I32, _I32, ctypes.POINTER(_I32), _I32, _F32, _F32,
                         _I32, _U64, ctypes.POINTER(_I32), ctypes.POINTER(sdsat_stats)], _I32),
     "sdsat_generate_tree": ([_VP, _I32, ctypes.POINTER(_I32), _I32, _I32, _I32, _I32, ctypes.POINTER(_I32), _I32,
@@ -59,6 +63,7 @@ _SIGNATURES = {
                                ctypes.POINTER(sdsat_stats)], _I32),
     "sdsat_kv_write": ([_VP, _I32, _I32, _I32, _VP, _VP, _VP], _I32),
     "sdsat_attention": ([_VP, _I32, _I32, _I32, _VP, _VP, _VP], _I32),
+    "sdsat_attention_shared": ([_VP, _I32, _I32, _I32, _I32, ctypes.POINTER(_I32), _VP, _VP, _VP], _I32),
     "sdsat_linear_packed_bytes": ([_I32, _I32, _I32], _SZ),
     "sdsat_linear_pack": ([_I32, _I32, _I32, _VP, _VP, _VP], _I32),
     "sdsat_linear_scratch_bytes": ([_I32, _I32, _I32], _SZ),
@@ -167,6 +172,36 @@ def sdsat_verify_nucleus(ctx, batch, q, logits, drafts, temperature, top_p, top_
                                       seed, _ptr(pos0), _ptr(tokens_out), _ptr(n_accept)), ctx)
 
 
+def _prefix_lens(batch, group, prefix_len):
+    """Host lengths of the groups' prefixes as a C array (one per group)."""
+    n = batch // group if group > 0 else 0
+    if len(prefix_len) != n:
+        raise ValueError("prefix_len must hold one length per group")
+    return (ctypes.c_int32 * max(1, n))(*prefix_len)
+
+
+def sdsat_forward_block_shared(ctx, batch, q, group, prefix_len, tokens, mask=None, logits=None):
+    """prefix_len: host lengths, one per group of `group` sequences."""
+    _check(lib().sdsat_forward_block_shared(ctx, batch, q, group, _prefix_lens(batch, group, prefix_len), _ptr(tokens),
+                                            _ptr(mask), _ptr(logits)), ctx)
+
+
+def sdsat_token_logprobs(ctx, batch, q, logits, tokens, temperature, n_top, logprob, entropy, top_ids=None,
+                         top_logprobs=None):
+    _check(lib().sdsat_token_logprobs(ctx, batch, q, _ptr(logits), _ptr(tokens), temperature, n_top, _ptr(logprob),
+                                      _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs)), ctx)
+
+
+def sdsat_kv_reorder(ctx, batch, src, first_slot=0):
+    _check(lib().sdsat_kv_reorder(ctx, batch, _ptr(src), first_slot), ctx)
+
+
+def sdsat_cache_ptr(ctx, layer):
+    k, v = ctypes.c_void_p(), ctypes.c_void_p()
+    _check(lib().sdsat_cache_ptr(ctx, layer, ctypes.byref(k), ctypes.byref(v)), ctx)
+    return k.value, v.value
+
+
 def sdsat_commit_kv(ctx, batch, q, n_commit, rows=None):
     _check(lib().sdsat_commit_kv(ctx, batch, q, _ptr(n_commit), _ptr(rows)), ctx)
 
@@ -210,6 +245,12 @@ def sdsat_kv_write(ctx, layer, batch, n, k, v, pos):
 
 def sdsat_attention(ctx, layer, batch, q, qin, mask, out):
     _check(lib().sdsat_attention(ctx, layer, batch, q, _ptr(qin), _ptr(mask), _ptr(out)), ctx)
+
+
+def sdsat_attention_shared(ctx, layer, batch, q, group, prefix_len, qin, mask, out):
+    """prefix_len: host lengths, one per group of `group` sequences."""
+    _check(lib().sdsat_attention_shared(ctx, layer, batch, q, group, _prefix_lens(batch, group, prefix_len), _ptr(qin),
+                                        _ptr(mask), _ptr(out)), ctx)
 
 
 def sdsat_linear_packed_bytes(dtype, N, K) -> int:
@@ -290,6 +331,28 @@ class Context:
         out = np.zeros(self.cfg.max_batch, np.int32)
         _hip_memcpy_d2h(out, sdsat_cache_len_ptr(self.handle))
         return out
+
+    def cache(self):
+        """The cache in place, as device views of the workspace: K [layers, max_batch, heads, slots, head_dim],
+        V [layers, max_batch, heads, slots / 32, 2, 4, 4, head_dim] (the key 16a + 4g + r of a page at [a, g, r]) and
+        the committed lengths [max_batch] (to be read: sdsat_set_cache_len writes them)."""
+        import torch
+        c = self.cfg
+        dt = torch.bfloat16 if c.dtype == DTYPE_BF16 else torch.float32
+        pages = (c.max_ctx + 31) // 32
+        dh, bh = c.head_dim, c.max_batch * c.n_heads
+
+        def view(ptr, dtype, shape, strides):
+            at = (ptr - self.workspace.data_ptr()) // dtype.itemsize
+            whole = self.workspace[: self.workspace.numel() // 4 * 4].view(dtype)
+            return whole.as_strided(shape, strides, whole.storage_offset() + at)
+
+        k, v = sdsat_cache_ptr(self.handle, 0)
+        page, row, layer = 32 * dh, 32 * dh * pages, 32 * dh * pages * bh
+        lead, lead_strides = (c.n_layers, c.max_batch, c.n_heads), (layer, row * c.n_heads, row)
+        return (view(k, dt, lead + (32 * pages, dh), lead_strides + (dh, 1)),
+                view(v, dt, lead + (pages, 2, 4, 4, dh), lead_strides + (page, 4, 8, 1, 32)),
+                view(sdsat_cache_len_ptr(self.handle), torch.int32, (c.max_batch,), (1,)))
 
 
 _hip = None

@@ -16,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsdsat.so")
-SOURCES = ["gemm.hip", "attention.hip", "verify.hip", "misc.hip", "prefill.hip", "prefill_gemm.hip", "noalloc.hip", "api.cpp"]
+SOURCES = ["gemm.hip", "attention.hip", "attention_shared.hip", "verify.hip", "logprobs.hip", "misc.hip", "reorder.hip",
+           "prefill.hip", "prefill_gemm.hip", "noalloc.hip", "api.cpp"]
 ARCH = "gfx950"
 
 

@@ -11,7 +11,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsdsat_hostsan.so")
-KERNEL_OBJECTS = ["gemm.o", "attention.o", "verify.o", "misc.o", "prefill.o", "prefill_gemm.o", "noalloc.o"]
+KERNEL_OBJECTS = ["gemm.o", "attention.o", "attention_shared.o", "verify.o", "logprobs.o", "misc.o", "reorder.o", "prefill.o",
+                  "prefill_gemm.o", "noalloc.o"]
 ROCM = "/opt/rocm"
 
 

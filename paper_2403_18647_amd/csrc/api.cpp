@@ -3,6 +3,7 @@
 // generation loop (Section 2.1).  Declared in include/sdsat.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <chrono>
 #include <cmath>
 #include <cstdio>
@@ -120,6 +121,11 @@ struct sdsat_ctx {
     size_t attn_part_floats = 0;
     int* attn_ctr = nullptr;      // attention split arrival counters (zero between launches)
     float* gemm_part = nullptr;   // partial rows of split residual GEMMs
+    float* shared_part = nullptr; // parts of shared-prefix attention
+    size_t shared_part_floats = 0;
+    int* reorder_steps = nullptr; // the copy list of a cache reordering
+    void* lp_part = nullptr;      // log probabilities: results of the chunks of a row, and (zero between launches) how
+    int* lp_ctr = nullptr;        // many have arrived
     int* cache_len = nullptr; int* err_flag = nullptr; int* verify_cnt = nullptr;
     unsigned long long* verify_best = nullptr;   // greedy verification: each row's best so far (zero between launches)
     // generation buffers
@@ -167,6 +173,16 @@ int fail(sdsat_ctx* c, int code, const std::string& msg) {
             return fail((ctx), SDSAT_EDEVICE, std::string(#expr) + ": " + hipGetErrorString(e_)); \
     } while (0)
 
+// The context's device is the current one while this lives (the caller's may be another).
+struct DeviceScope {
+    int before = -1;
+    explicit DeviceScope(int device) {
+        int now = device;
+        if (hipGetDevice(&now) == hipSuccess && now != device && hipSetDevice(device) == hipSuccess) before = now;
+    }
+    ~DeviceScope() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
 // Carve every device buffer of a context (ctx may be a measuring dummy).
 void carve(sdsat_ctx* c, Carver& cv) {
     const Dims& D = c->D;
@@ -201,6 +217,11 @@ void carve(sdsat_ctx* c, Carver& cv) {
                                      gemm_resid_part_bytes(D.nt_down, D.ks_f, rows));
         c->gemm_part = part ? (float*)cv.take(part) : nullptr;
     }
+    c->shared_part_floats = shared_partial_floats_most(D.maxB, D.H, D.maxQ, D.Dh);
+    c->shared_part = (float*)cv.take(c->shared_part_floats * 4);
+    c->reorder_steps = (int*)cv.take((2 + 6 * (size_t)D.maxB) * 4);
+    c->lp_part = cv.take(logprob_part_bytes(D.maxM, D.V));
+    c->lp_ctr = (int*)cv.take((size_t)D.maxM * 4);
     c->cache_len = (int*)cv.take((size_t)D.maxB * 4);
     c->err_flag = (int*)cv.take(4);
     c->verify_cnt = (int*)cv.take((size_t)D.maxB * 4);
@@ -316,10 +337,29 @@ int fits(sdsat_ctx* c, int B, int q, bool* ok) {
     return SDSAT_OK;
 }
 
+// Groups of sequences that share a prefix: whole 32-slot pages of it, by group.
+struct Share { int group; int pages[kMaxShareGroups]; };
+
 // out: float rows (out_f32), or elements in fragment order of out_rows rows (B*q, or that rounded up to 16)
 int attention_layer(sdsat_ctx* c, int layer, int B, int q, const uint64_t* mask, const float* qbuf, void* out,
-                    int out_f32, int ldo, int out_rows) {
+                    int out_f32, int ldo, int out_rows, const Share* share) {
     const Dims& D = c->D;
+    if (share && share->group > 1) {   // a group of one holds its whole cache itself
+        const SharedPlan p = plan_shared(B, share->group, D.H, q, D.dtype, share->pages, max_hint(c, B), D.S);
+        if (shared_partial_floats(p, B, q, D.H, D.Dh) > c->shared_part_floats)   // sized at init for every plan
+            return fail(c, SDSAT_EDEVICE, "shared attention plan needs more parts than the workspace holds");
+        SharedArgs a{};
+        a.at.qbuf = qbuf; a.at.kc = layer_k(c, layer); a.at.vc = layer_v(c, layer); a.at.cache_len = c->cache_len;
+        a.at.mask = mask; a.at.B = B; a.at.q = q; a.at.H = D.H; a.at.S_max = D.S;
+        a.at.scale = (float)(1.4426950408889634 / std::sqrt((double)D.Dh));
+        a.at.out = out; a.at.out_f32 = out_f32; a.at.ldo = ldo; a.at.out_rows = out_rows; a.at.err = c->err_flag;
+        a.group = share->group; a.part = c->shared_part;
+        std::copy(share->pages, share->pages + B / share->group, a.pages);
+        hipEvent_t e0, e1;
+        prof_pair(c, PK_ATTN, &e0, &e1);
+        HIPCHK(c, launch_attention_shared(D.dtype, D.Dh, p, a, c->stream, e0, e1));
+        return SDSAT_OK;
+    }
     if (!mask && q > kAttnSplitRows && attention_rows_supported(D.dtype, D.Dh)) {   // prefill: 64-row tiles
         AttnArgs a{};
         a.qbuf = qbuf; a.kc = layer_k(c, layer); a.vc = layer_v(c, layer); a.cache_len = c->cache_len;
@@ -393,7 +433,7 @@ int big_gemm_swiglu(sdsat_ctx* c, int M, const void* A, const void* w_gate, cons
 // Block forward of a large block (B*q > kSkinnyRows rows, chain mask): linear layers as matrix-core GEMMs
 // (QKV and gate | up with their RoPE / cache and SwiGLU epilogues), the rest in
 // row-wise kernels that round where the skinny path rounds.
-int large_block_impl(sdsat_ctx* c, int B, int q, const int32_t* tokens, float* logits) {
+int large_block_impl(sdsat_ctx* c, int B, int q, const int32_t* tokens, float* logits, const Share* share) {
     const Dims& D = c->D;
     const int M = B * q;
     const float eps = c->cfg.rms_eps;
@@ -407,7 +447,7 @@ int large_block_impl(sdsat_ctx* c, int B, int q, const int32_t* tokens, float* l
         const void* const* w = c->w_src.data() + 1 + 9 * l;   // attn_norm, wq, wk, wv, wo, ffn_norm, wg, wu, wd
         int rc = big_gemm_qkv(c, B, q, c->hbuf, w, l);
         if (rc) return rc;
-        rc = attention_layer(c, l, B, q, nullptr, (const float*)c->qbuf, c->obuf, 0, D.d_pad, M16);
+        rc = attention_layer(c, l, B, q, nullptr, (const float*)c->qbuf, c->obuf, 0, D.d_pad, M16, share);
         if (rc) return rc;
         const size_t y_part = (size_t)D.maxM * D.d;   // offset between split-K partials in c_y
         int parts = 1;
@@ -431,10 +471,11 @@ int large_block_impl(sdsat_ctx* c, int B, int q, const int32_t* tokens, float* l
     return SDSAT_OK;
 }
 
-int forward_block_impl(sdsat_ctx* c, int B, int q, const int32_t* tokens, const uint64_t* mask, float* logits) {
+int forward_block_impl(sdsat_ctx* c, int B, int q, const int32_t* tokens, const uint64_t* mask, float* logits,
+                       const Share* share = nullptr) {
     const Dims& D = c->D;
     const int M = B * q;
-    if (M > kSkinnyRows) return large_block_impl(c, B, q, tokens, logits);
+    if (M > kSkinnyRows) return large_block_impl(c, B, q, tokens, logits, share);
     // The GEMMs behind an RMSNorm read X either as the float rows x o g, scaled
     // and rounded at the matrix-core input (one-row blocks; QKV up to 8 rows),
     // or as those rows rounded once by rms_rows: every workgroup re-reads X.
@@ -478,7 +519,7 @@ int forward_block_impl(sdsat_ctx* c, int B, int q, const int32_t* tokens, const 
         a.rope = c->rope;
         rc = run_gemm(c, PK_QKV, EP_QKV, M, D.nt_qkv, D.ks_d, 3 * D.d, D.d, c->w_qkv[l], a);
         if (rc) return rc;
-        rc = attention_layer(c, l, B, q, mask, (const float*)c->qbuf, c->obuf, 0, D.d_pad, M);
+        rc = attention_layer(c, l, B, q, mask, (const float*)c->qbuf, c->obuf, 0, D.d_pad, M, share);
         if (rc) return rc;
         GemmArgs o{};
         o.xa = c->obuf; o.ldx = D.d_pad; o.resid = c->x; o.ldy = D.d; o.xg_out = c->xg; o.ldxg = D.d_pad;
@@ -510,6 +551,22 @@ int forward_block_impl(sdsat_ctx* c, int B, int q, const int32_t* tokens, const 
     return SDSAT_OK;
 }
 
+// Groups of `group` sequences and their prefixes (slots), as whole pages.
+int check_share(sdsat_ctx* c, int B, int group, const int32_t* h_prefix_len, Share* share) {
+    if (group < 1 || B % group) return fail(c, SDSAT_EINVAL, "batch must be a multiple of group");
+    if (B / group > kMaxShareGroups) return fail(c, SDSAT_EUNSUPPORTED, "at most 64 groups share prefixes in one call");
+    if (!h_prefix_len) return fail(c, SDSAT_EINVAL, "h_prefix_len is NULL");
+    share->group = group;
+    for (int g = 0; g < B / group; ++g) {
+        if (h_prefix_len[g] < 0) return fail(c, SDSAT_EINVAL, "negative prefix length");
+        for (int b = g * group; b < (g + 1) * group; ++b)   // len_hint: an upper bound of the committed length
+            if (h_prefix_len[g] > c->len_hint[b])
+                return fail(c, SDSAT_ECAPACITY, "shared prefix longer than a sequence's committed slots");
+        share->pages[g] = h_prefix_len[g] / 32;
+    }
+    return SDSAT_OK;
+}
+
 int read_err_flag(sdsat_ctx* c) {
     int h = 0;
     HIPCHK(c, hipMemcpyAsync(&h, c->err_flag, 4, hipMemcpyDeviceToHost, c->stream));
@@ -519,7 +576,9 @@ int read_err_flag(sdsat_ctx* c) {
         return fail(c, SDSAT_EDATA, (h & 1)   ? "token id out of range in a block"
                                     : (h & 2) ? "invalid commit rows"
                                     : (h & 4) ? "cache capacity exceeded"
-                                              : "attention launched for a shorter cache than committed");
+                                    : (h & 16) ? "shared prefix longer than a sequence's committed slots"
+                                    : (h & 32) ? "source sequence out of range in a reordering"
+                                               : "attention launched for a shorter cache than committed");
     }
     return SDSAT_OK;
 }
@@ -646,6 +705,7 @@ int sdsat_init(const sdsat_config* cfg, const void* const* weights, int32_t n_we
         // verify_cnt and verify_best: neighbours in the workspace, one launch
         (void)launch_fill_i32(c->verify_cnt, (size_t)((int*)(c->verify_best + D.maxM) - c->verify_cnt), 0, c->stream);
         (void)launch_fill_i32(c->attn_ctr, attention_counter_ints(D.maxB, D.H, D.maxQ), 0, c->stream);
+        (void)launch_fill_i32(c->lp_ctr, (size_t)D.maxM, 0, c->stream);
         (void)launch_fill_i32(c->cache_len, D.maxB, 0, c->stream);
         (void)launch_fill_i32(c->err_flag, 1, 0, c->stream);
         if (hipStreamSynchronize(c->stream) != hipSuccess) {
@@ -704,6 +764,25 @@ int sdsat_forward_block(sdsat_ctx* c, int32_t batch, int32_t q, const int32_t* d
     return forward_block_impl(c, batch, q, d_tokens, d_ancestor_mask, d_logits);
 }
 
+int sdsat_forward_block_shared(sdsat_ctx* c, int32_t batch, int32_t q, int32_t group, const int32_t* h_prefix_len,
+                               const int32_t* d_tokens, const uint64_t* d_ancestor_mask, float* d_logits) {
+    if (!c) return fail(nullptr, SDSAT_EINVAL, "ctx is NULL");
+    const DeviceScope scope(c->device);
+    int rc = check_block_args(c, batch, q);
+    if (rc) return rc;
+    if (!d_tokens) return fail(c, SDSAT_EINVAL, "d_tokens is NULL");
+    if (batch * q > kSkinnyRows && d_ancestor_mask)
+        return fail(c, SDSAT_EUNSUPPORTED, "ancestor masks need batch * q <= 64");
+    Share share;
+    rc = check_share(c, batch, group, h_prefix_len, &share);
+    if (rc) return rc;
+    bool ok = false;
+    rc = fits(c, batch, q, &ok);
+    if (rc) return rc;
+    if (!ok) return fail(c, SDSAT_ECAPACITY, "cache_len + q exceeds max_ctx");
+    return forward_block_impl(c, batch, q, d_tokens, d_ancestor_mask, d_logits, &share);
+}
+
 int sdsat_verify_greedy(sdsat_ctx* c, int32_t batch, int32_t q, const float* d_logits, const int32_t* d_drafts,
                         int32_t* d_tokens_out, int32_t* d_n_accept) {
     if (!c) return fail(nullptr, SDSAT_EINVAL, "ctx is NULL");
@@ -728,6 +807,50 @@ int sdsat_verify_nucleus(sdsat_ctx* c, int32_t batch, int32_t q, const float* d_
     if (!(top_p > 0.f) || std::isnan(temperature)) return fail(c, SDSAT_EINVAL, "top_p must be > 0");
     HIPCHK(c, launch_verify_nucleus(d_logits, batch, q, c->D.V, d_drafts, q - 1, temperature, top_p, top_k, seed,
                                     d_pos0, d_tokens_out, d_n_accept, c->verify_cnt, c->stream));
+    return SDSAT_OK;
+}
+
+int sdsat_token_logprobs(sdsat_ctx* c, int32_t batch, int32_t q, const float* d_logits, const int32_t* d_tokens,
+                         float temperature, int32_t n_top, float* d_logprob, float* d_entropy, int32_t* d_top_ids,
+                         float* d_top_logprobs) {
+    if (!c) return fail(nullptr, SDSAT_EINVAL, "ctx is NULL");
+    const DeviceScope scope(c->device);
+    int rc = check_block_args(c, batch, q);
+    if (rc) return rc;
+    if (!d_logits || (d_logprob && !d_tokens)) return fail(c, SDSAT_EINVAL, "NULL logits, or tokens with logprob");
+    if (!(temperature > 0.f) || !std::isfinite(temperature))
+        return fail(c, SDSAT_EINVAL, "temperature must be positive and finite");
+    if (n_top < 0 || n_top > kMaxTop || n_top > c->D.V) return fail(c, SDSAT_EINVAL, "n_top must be 0..32 and at most V");
+    if (n_top && (!d_top_ids || !d_top_logprobs)) return fail(c, SDSAT_EINVAL, "NULL top_ids or top_logprobs with n_top");
+    if ((long)logprob_chunks(c->D.V) * n_top > kMaxTopKeys)
+        return fail(c, SDSAT_EUNSUPPORTED, "n_top too large for this vocabulary (V / 8192 * n_top <= 4096)");
+    if (!d_logprob && !d_entropy && !n_top) return SDSAT_OK;
+    HIPCHK(c, launch_token_logprobs(d_logits, batch * q, c->D.V, d_tokens, temperature, n_top, d_logprob, d_entropy, d_top_ids,
+                                    d_top_logprobs, c->lp_part, c->lp_ctr, c->err_flag, c->stream));
+    return SDSAT_OK;
+}
+
+int sdsat_kv_reorder(sdsat_ctx* c, int32_t batch, const int32_t* d_src, int32_t first_slot) {
+    if (!c) return fail(nullptr, SDSAT_EINVAL, "ctx is NULL");
+    const DeviceScope scope(c->device);
+    const Dims& D = c->D;
+    if (batch < 1 || batch > D.maxB) return fail(c, SDSAT_EINVAL, "batch out of range");
+    if (D.maxB > kReorderMaxBatch) return fail(c, SDSAT_EUNSUPPORTED, "reordering needs max_batch <= 1024");
+    if (!d_src) return fail(c, SDSAT_EINVAL, "d_src is NULL");
+    if (first_slot < 0 || first_slot > D.S) return fail(c, SDSAT_EINVAL, "first_slot out of range");
+    const int most = max_hint(c, D.maxB);
+    HIPCHK(c, launch_reorder(D.esz, c->kc, c->vc, c->layer_elems, D.L, batch, D.maxB, D.H, D.Dh, D.S, c->cache_len, most, d_src,
+                             first_slot, c->reorder_steps, c->err_flag, c->stream));
+    for (int b = 0; b < batch; ++b) c->len_hint[b] = most;
+    return SDSAT_OK;
+}
+
+int sdsat_cache_ptr(const sdsat_ctx* c, int32_t layer, void** d_k, void** d_v) {
+    if (!c) return fail(nullptr, SDSAT_EINVAL, "ctx is NULL");
+    if (layer < 0 || layer >= c->D.L || !d_k || !d_v)
+        return fail(const_cast<sdsat_ctx*>(c), SDSAT_EINVAL, "layer out of range, or NULL d_k or d_v");
+    *d_k = layer_k(const_cast<sdsat_ctx*>(c), layer);
+    *d_v = layer_v(const_cast<sdsat_ctx*>(c), layer);
     return SDSAT_OK;
 }
 
@@ -992,7 +1115,27 @@ int sdsat_attention(sdsat_ctx* c, int32_t layer, int32_t batch, int32_t q, const
     if (rc) return rc;
     if (!ok) return fail(c, SDSAT_ECAPACITY, "cache_len + q exceeds max_ctx");
     HIPCHK(c, hipMemcpyAsync(c->qbuf, d_q, (size_t)batch * q * D.d * 4, hipMemcpyDeviceToDevice, c->stream));
-    return attention_layer(c, layer, batch, q, d_ancestor_mask, (const float*)c->qbuf, d_out, 1, D.d, batch * q);
+    return attention_layer(c, layer, batch, q, d_ancestor_mask, (const float*)c->qbuf, d_out, 1, D.d, batch * q, nullptr);
+}
+
+int sdsat_attention_shared(sdsat_ctx* c, int32_t layer, int32_t batch, int32_t q, int32_t group,
+                           const int32_t* h_prefix_len, const float* d_q, const uint64_t* d_ancestor_mask, float* d_out) {
+    if (!c) return fail(nullptr, SDSAT_EINVAL, "ctx is NULL");
+    const DeviceScope scope(c->device);
+    int rc = check_block_args(c, batch, q);
+    if (rc) return rc;
+    const Dims& D = c->D;
+    if (layer < 0 || layer >= D.L || !d_q || !d_out) return fail(c, SDSAT_EINVAL, "bad attention arguments");
+    if (q > kAttnSplitRows && d_ancestor_mask) return fail(c, SDSAT_EUNSUPPORTED, "ancestor masks need q <= 64");
+    Share share;
+    rc = check_share(c, batch, group, h_prefix_len, &share);
+    if (rc) return rc;
+    if (group == 1) return sdsat_attention(c, layer, batch, q, d_q, d_ancestor_mask, d_out);
+    bool ok = false;
+    rc = fits(c, batch, q, &ok);
+    if (rc) return rc;
+    if (!ok) return fail(c, SDSAT_ECAPACITY, "cache_len + q exceeds max_ctx");
+    return attention_layer(c, layer, batch, q, d_ancestor_mask, d_q, d_out, 1, D.d, batch * q, &share);
 }
 
 size_t sdsat_linear_packed_bytes(int32_t dtype, int32_t N, int32_t K) {

@@ -139,6 +139,38 @@ inline bool attention_rows_supported(int dtype, int head_dim) { return head_dim 
 hipError_t launch_attention_rows(int dtype, int head_dim, const AttnArgs& a, hipStream_t s,
                                  hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);
 
+// Attention of groups of `group` sequences whose first pages[g] 32-slot pages (shared, whole) lie in the cache of the
+// group's first sequence; `at` as above with scale in units of log 2 (times log2 e), its splits, per_split, cols, part
+// and counter unused.  The launch fills the rest from its plan.
+constexpr int kMaxShareGroups = 64;
+constexpr int kSharedParts = 512;      // workgroups the shared pages (one row tile) and the own pages are cut into, about
+constexpr int kSharedMaxParts = 32;    // parts of a prefix, at most
+constexpr int kSharedMaxOwn = 8;       // parts of a sequence's own slots, at most
+struct SharedArgs {
+    AttnArgs at;
+    int group;
+    int pages[kMaxShareGroups];
+    float* part;                       // [B*q][H][slots][Dh + 4]: O to the part's maximum, the maximum, the sum
+    int chunk, prefix_parts, own_chunk, own_parts, slots, tiles, prefix_grid;
+};
+struct SharedPlan {
+    bool whole;                        // blocks of more than kAttnSplitRows rows: no parts
+    int rt, chunk, prefix_parts, own_chunk, own_parts, slots, tiles, own_tiles, prefix_grid, grid;
+};
+SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pages, int max_len, int S_max);
+size_t shared_partial_floats(const SharedPlan& p, int B, int q, int H, int head_dim);
+size_t shared_partial_floats_most(int B_max, int H, int q_max, int head_dim);
+hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p, SharedArgs a, hipStream_t s,
+                                   hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);
+
+// ---------------------------------------------------------------- cache reordering
+// sequence b < batch continues from sequence src[b] (any of the `all`, -1: none): whole pages from first_slot's on,
+// up to max_len at the most, and the lengths.  steps: 2 + 6 * all ints
+constexpr int kReorderMaxBatch = 1024;
+hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n_layers, int batch, int all, int H, int Dh,
+                          int S_max, int* cache_len, int max_len, const int* src, int first_slot, int* steps, int* err,
+                          hipStream_t s);
+
 // ---------------------------------------------------------------- misc kernels
 hipError_t launch_embed(int dtype, const void* embed, int n_rows_emb, int d, const int* tokens, int M,
                         float* x, float* xg, const float* gain, int ldxg, float* ssq, int n_ssq, int* err,
@@ -236,6 +268,15 @@ hipError_t launch_verify_nucleus(const float* logits, int B, int q, int V, const
                                  float temperature, float top_p, int top_k, uint64_t seed, const int* pos0,
                                  int* tokens_out, int* n_accept, int* counter, hipStream_t s,
                                  const int* row_depth = nullptr);
+
+// Log probabilities of tokens (negative: none, 0 is written) under logits rows at a temperature, the rows' entropies
+// and n_top alternatives.  lp, ent: [M] or null; part: logprob_part_bytes; counter [M]: zero between launches
+constexpr int kMaxTop = 32;
+constexpr int kMaxTopKeys = 4096;      // chunks of a row times n_top, at most
+int logprob_chunks(int V);
+size_t logprob_part_bytes(int M, int V);
+hipError_t launch_token_logprobs(const float* logits, int M, int V, const int* tokens, float temperature, int n_top, float* lp,
+                                 float* ent, int* ids, float* top_lp, void* part, int* counter, int* err, hipStream_t s);
 
 // draft tree of width w over draft step 1's rows (k adaptive rows): q2 = 1 + k*w block rows
 constexpr int kMaxTreeWidth = 8;

@@ -1,0 +1,301 @@
+"""sdsat_attention_shared against float64 softmax attention over the same keys and values: groups and ragged lengths,
+prefixes that end inside a page or hold none, tree masks, empty rows, what stands in slots that no row sees, block-size
+invariance, streams and captured graphs."""
+import math
+
+import pytest
+import torch
+
+from operator_helpers import context, device_error
+from paper_2403_18647_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def case(dtype, heads, dh, group, prefix, own, q, slots=0, seed=0, spread=1.0):
+    """A context whose cache holds groups of `group` sequences with the given prefixes and own lengths (the block's rows
+    in place), and each sequence's whole key list [heads, prefix + own + q, dh] in float64."""
+    n = len(prefix) * group
+    slots = slots or max(prefix) + max(own) + q
+    ctx = context(heads, dh, dtype, 1, n, slots, q)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    k, v, _ = ctx.cache()
+    vflat = torch.zeros_like(k[0])
+    keys, vals = [], []
+    for b in range(n):
+        i = b // group
+        p, total = prefix[i], prefix[i] + own[b] + q
+        mine = [spread * torch.randn((heads, total, dh), generator=g, device="cuda").to(k.dtype) for _ in range(2)]
+        if b % group:
+            for t, o in zip(mine, (keys, vals)):
+                t[:, :p] = o[i * group][:, :p].to(k.dtype)
+        lo = 0 if b % group == 0 else p // 32 * 32
+        k[0, b, :, lo:total] = mine[0][:, lo:]
+        vflat[b, :, lo:total] = mine[1][:, lo:]
+        keys.append(mine[0].double())
+        vals.append(mine[1].double())
+    v[0].copy_(vflat.view(v[0].shape))
+    B.sdsat_set_cache_len(ctx.handle, [prefix[b // group] + own[b] for b in range(n)])
+    x = torch.randn((n * q, heads * dh), generator=g, device="cuda")
+    return ctx, keys, vals, x
+
+
+def reference(keys, vals, x, q, sees):
+    """Outputs and, for each, how far a float32 computation with value-and-remainder operands may be off.
+
+    A score is a sum of dh products q k / sqrt(dh): each operand pair holds its float to 2^-18 (bf16 models; the
+    remainder's own rounding), each float32 addition rounds by 2^-24 of at most the sum of |q k|; so it errs by at most
+    e = (2^-18 + (dh + 4) 2^-24) max_key sum |q k| / sqrt(dh).  exp turns e into the relative error of a weight (and adds
+    its own 2^-22 and, raised up to 2^8, nothing), the pair for P 2^-18; numerator and denominator err alike, so an output
+    is off by at most (2 e + 2^-16) sum p |v|, and float32 sums of n keys add n 2^-24 of it."""
+    heads, dh = keys[0].shape[0], keys[0].shape[2]
+    out, tol = [], []
+    for b, (k, v) in enumerate(zip(keys, vals)):
+        xb = x.view(len(keys), q, heads, dh)[b].double().transpose(0, 1).contiguous()
+        kt = k.transpose(1, 2).contiguous()
+        s = torch.matmul(xb, kt) / math.sqrt(dh)
+        e = (2.0 ** -18 + (dh + 4) * 2.0 ** -24) * (torch.matmul(xb.abs(), kt.abs()) / math.sqrt(dh)).amax(-1, keepdim=True)
+        p = s.masked_fill(~sees[b], -math.inf).softmax(-1).nan_to_num(0.0)
+        out.append(torch.matmul(p, v).transpose(0, 1).reshape(q, -1))
+        t = (2 * e + 2.0 ** -16 + k.shape[1] * 2.0 ** -24) * torch.matmul(p, v.abs())
+        tol.append(t.transpose(0, 1).reshape(q, -1))
+    return torch.cat(out), torch.cat(tol) + 1e-30
+
+
+def chain(keys, q):
+    return [torch.ones((q, k.shape[1]), dtype=torch.bool, device="cuda").tril(k.shape[1] - q) for k in keys]
+
+
+def run(ctx, group, prefix, q, x, mask=None):
+    out = torch.full_like(x, 7e7)
+    B.sdsat_attention_shared(ctx.handle, 0, len(prefix) * group, q, group, prefix, x, mask, out)
+    torch.cuda.synchronize()
+    return out
+
+
+def check(out, ref, tol):
+    off = (out.double() - ref).abs()
+    assert bool((off <= tol).all()), (float(off.max()), float((off / tol).max()))
+
+
+DECODE = [
+    # group, prefixes, own lengths, q
+    (2, [64], [0, 0], 1),                          # nothing but the block behind the prefix
+    (2, [0], [5, 40], 3),                          # no prefix at all
+    (2, [31], [1, 0], 2),                          # a prefix without a whole page
+    (3, [33], [7, 0, 31], 6),                      # one page; the rest in each sequence's own slots
+    (4, [100], [20, 3, 32, 150], 6),
+    (5, [640], [1, 2, 3, 4, 5], 11),               # 55 rows: a last tile of 7
+    (2, [96, 0, 257], [0, 9, 70, 33, 1, 64], 4),   # ragged groups
+    (16, [200], [3] * 16, 5),                      # 80 rows: more than one tile of rows
+    (8, [1000], [9, 700, 0, 64, 65, 31, 32, 33], 1),
+    (2, [2048], [500, 12], 64),                    # the longest block that is cut into parts
+]
+
+
+@pytest.mark.parametrize("group,prefix,own,q", DECODE)
+@pytest.mark.parametrize("dtype,heads,dh", [("bf16", 2, 128), ("bf16", 3, 64), ("fp32", 2, 64), ("fp32", 1, 128)])
+def test_decode_blocks(dtype, heads, dh, group, prefix, own, q):
+    ctx, keys, vals, x = case(dtype, heads, dh, group, prefix, own, q, seed=q)
+    ref, tol = reference(keys, vals, x, q, chain(keys, q))
+    check(run(ctx, group, prefix, q, x), ref, tol)
+    assert device_error(ctx) == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("heads,group,prefix,own,q", [
+    (32, 8, [1024], [150, 0, 31, 75, 20, 149, 3, 64], 6), (40, 4, [777, 1500], [5] * 8, 11), (32, 32, [300], [17] * 32, 2)])
+def test_model_heads(heads, group, prefix, own, q):
+    ctx, keys, vals, x = case("bf16", heads, 128, group, prefix, own, q, slots=2000)
+    ref, tol = reference(keys, vals, x, q, chain(keys, q))
+    check(run(ctx, group, prefix, q, x), ref, tol)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype,heads,dh", [("bf16", 2, 128), ("bf16", 2, 64), ("fp32", 2, 64), ("fp32", 1, 128)])
+@pytest.mark.parametrize("group,prefix,own,q", [(2, [100], [0, 0], 65), (3, [64], [40, 0, 3], 130), (2, [0], [0, 1], 100),
+                                                (2, [500, 31], [0, 0, 9, 0], 128)])
+def test_long_blocks(dtype, heads, dh, group, prefix, own, q):
+    ctx, keys, vals, x = case(dtype, heads, dh, group, prefix, own, q, seed=q)
+    ref, tol = reference(keys, vals, x, q, chain(keys, q))
+    check(run(ctx, group, prefix, q, x), ref, tol)
+    assert device_error(ctx) == 0
+    ctx.close()
+
+
+def test_a_very_long_prefix():
+    prefix, own, q = [70000], [3, 60], 2
+    ctx, keys, vals, x = case("bf16", 2, 128, 2, prefix, own, q)
+    ref, tol = reference(keys, vals, x, q, chain(keys, q))
+    check(run(ctx, 2, prefix, q, x), ref, tol)
+    ctx.close()
+
+
+def test_large_scores():
+    """Scores of about +-100: a maximum that is raised many times, weights far below it."""
+    prefix, own, q = [300], [33, 8], 6
+    ctx, keys, vals, x = case("bf16", 2, 128, 2, prefix, own, q, spread=3.0)
+    x = x * 3
+    ref, tol = reference(keys, vals, x, q, chain(keys, q))
+    check(run(ctx, 2, prefix, q, x), ref, tol)
+    # rising scores: every key larger than the ones before
+    k, _, _ = ctx.cache()
+    ramp = torch.arange(k.shape[3], device="cuda") * 0.05
+    k.copy_(ramp[:, None].expand(k.shape[3], k.shape[4]))
+    k[0, 1, :, 320:].mul_(-1)
+    kb = [k[0, 0, :, :keys[0].shape[1]].double()]
+    kb.append(torch.cat([kb[0][:, :288], k[0, 1, :, 288:keys[1].shape[1]].double()], 1))
+    ref, tol = reference(kb, vals, x, q, chain(kb, q))
+    check(run(ctx, 2, prefix, q, x), ref, tol)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("fp32", 64)])
+@pytest.mark.parametrize("prefix,own", [([64], [0, 35]), ([40], [20, 3]), ([0], [0, 1])])
+def test_tree_masks(dtype, dh, prefix, own):
+    q = 7
+    rows = [0b1, 0b11, 0b111, 0b1111, 0b10001, 0b100011, 0b1000111]
+    ctx, keys, vals, x = case(dtype, 2, dh, 2, prefix, own, q)
+    sees = []
+    for k in keys:
+        see = torch.ones((q, k.shape[1]), dtype=torch.bool, device="cuda")
+        see[:, -q:] = torch.tensor([[r >> j & 1 for j in range(q)] for r in rows], device="cuda").bool()
+        sees.append(see)
+    mask = torch.tensor(rows * 2, dtype=torch.int64, device="cuda")
+    ref, tol = reference(keys, vals, x, q, sees)
+    check(run(ctx, 2, prefix, q, x, mask), ref, tol)
+    ctx.close()
+
+
+def test_a_row_that_sees_no_key_gives_zeros():
+    ctx, keys, vals, x = case("bf16", 2, 64, 2, [0], [0, 0], 3)
+    mask = torch.tensor([1, 0, 7, 0, 2, 0], dtype=torch.int64, device="cuda")
+    out = run(ctx, 2, [0], 3, x, mask)
+    assert not out[1].any() and not out[3].any() and not out[5].any()
+    sees = [torch.tensor([[1, 0, 0], [0, 0, 0], [1, 1, 1]], device="cuda").bool(),
+            torch.tensor([[0, 0, 0], [0, 1, 0], [0, 0, 0]], device="cuda").bool()]
+    ref, tol = reference(keys, vals, x, 3, sees)
+    check(out, ref, tol)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("fp32", 64), ("bf16", 64)])
+@pytest.mark.parametrize("q", [5, 70])
+@pytest.mark.parametrize("junk", [math.inf, -math.inf, math.nan, 3e38])
+def test_slots_that_no_row_sees(dtype, dh, q, junk):
+    """Whatever stands past a sequence's rows, or in the prefix's pages of the sequences that share it."""
+    prefix, own = [70], [3, 40]
+    ctx, keys, vals, x = case(dtype, 2, dh, 2, prefix, own, q, slots=200)
+    want = run(ctx, 2, prefix, q, x)
+    k, v, _ = ctx.cache()
+    dead = torch.ones((2, k.shape[3]), dtype=torch.bool, device="cuda")
+    for b in range(2):
+        dead[b, (0 if b == 0 else 64):prefix[0] + own[b] + q] = False
+    k.masked_fill_(dead[None, :, None, :, None], junk)
+    v.masked_fill_(dead.view(2, -1, 2, 4, 4)[None, :, None, :, :, :, :, None], junk)
+    assert torch.equal(run(ctx, 2, prefix, q, x), want)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype,dh,prefix,own", [("bf16", 128, 500, 33), ("bf16", 64, 64, 31), ("fp32", 64, 300, 100)])
+def test_a_row_does_not_depend_on_its_block(dtype, dh, prefix, own):
+    """Row r of a block is bitwise the one-row block at the same position, whatever the block's size."""
+    q, group = 40, 4
+    ctx, keys, vals, x = case(dtype, 2, dh, group, [prefix], [own] * group, q)
+    whole = run(ctx, group, [prefix], q, x).view(group, q, -1)
+    for rows in (1, 5, 17):
+        for r in (0, 1, 13, 23):
+            B.sdsat_set_cache_len(ctx.handle, [prefix + own + r] * group)
+            part = x.view(group, q, -1)[:, r:r + rows].contiguous().view(group * rows, -1)
+            got = run(ctx, group, [prefix], rows, part).view(group, rows, -1)
+            assert torch.equal(got, whole[:, r:r + rows]), (rows, r)
+    ctx.close()
+
+
+def test_repeated_calls_are_bitwise_alike_and_groups_of_one_are_the_plain_attention():
+    ctx, keys, vals, x = case("bf16", 4, 128, 4, [300], [5, 60, 0, 31], 6)
+    want = run(ctx, 4, [300], 6, x)
+    for _ in range(3):
+        assert torch.equal(run(ctx, 4, [300], 6, x), want)
+    plain = torch.empty_like(x)
+    B.sdsat_attention(ctx.handle, 0, 4, 6, x, None, plain)
+    assert torch.equal(run(ctx, 1, [300, 10, 0, 31], 6, x), plain)
+    ctx.close()
+
+
+def test_queries_at_float_alignment():
+    ctx, keys, vals, x = case("bf16", 2, 128, 2, [100], [5, 9], 3)
+    want = run(ctx, 2, [100], 3, x)
+    room = torch.empty(x.numel() + 1, device="cuda")
+    odd = room[1:].view(x.shape)
+    odd.copy_(x)
+    put = torch.empty(x.numel() + 1, device="cuda")
+    B.sdsat_attention_shared(ctx.handle, 0, 2, 3, 2, [100], odd, None, put[1:])
+    torch.cuda.synchronize()
+    assert torch.equal(put[1:].view(x.shape), want)
+    ctx.close()
+
+
+def test_refusals():
+    ctx, keys, vals, x = case("bf16", 2, 64, 2, [64], [5, 9], 3, slots=300)
+    big = context(2, 64, "bf16", 1, 2, 300, 70)
+    B.sdsat_set_cache_len(big.handle, [64, 64])
+    xb = torch.zeros((140, 128), device="cuda")
+    mask = torch.ones(140, dtype=torch.int64, device="cuda")
+
+    def code(h, *a):
+        with pytest.raises(B.SdsatError) as e:
+            B.sdsat_attention_shared(h, *a)
+        return e.value.code
+    h = ctx.handle
+    assert code(h, 1, 2, 3, 2, [64], x, None, x) == -1            # layer
+    assert code(h, 0, 2, 3, 0, [], x, None, x) == -1              # no group
+    assert code(h, 0, 2, 3, 4, [], x, None, x) == -1              # batch is not a multiple
+    assert code(h, 0, 4, 3, 2, [64, 64], x, None, x) == -4        # batch
+    assert code(h, 0, 2, 4, 2, [64], x, None, x) == -4            # rows
+    assert code(h, 0, 2, 3, 2, [-1], x, None, x) == -1            # negative prefix
+    assert code(h, 0, 2, 3, 2, [70], x, None, x) == -4            # longer than sequence 0
+    assert code(h, 0, 2, 3, 2, [64], None, None, x) == -1
+    assert code(h, 0, 2, 3, 2, [64], x, None, None) == -1
+    assert code(big.handle, 0, 2, 70, 2, [64], xb, mask, xb) == -5   # masks of a long block
+    B.sdsat_set_cache_len(h, [318, 318])   # of 320 slots
+    assert code(h, 0, 2, 3, 2, [64], x, None, x) == -4            # past the slots
+    ctx.close()
+    big.close()
+
+
+def test_a_prefix_longer_than_the_device_s_length_is_reported():
+    """The host's bound allows it (a commit of fewer rows than the block had), the device knows better."""
+    ctx, keys, vals, x = case("bf16", 2, 64, 2, [64], [20, 20], 3, slots=300)
+    B.sdsat_reset(ctx.handle, 2)
+    for _ in range(30):
+        B.sdsat_commit_kv(ctx.handle, 2, 3, torch.ones(2, dtype=torch.int32, device="cuda"))   # bound 90, length 30
+    run(ctx, 2, [64], 3, x)
+    assert device_error(ctx) == -6
+    ctx.close()
+
+
+@pytest.mark.parametrize("q", [6, 66])
+def test_captured_on_a_stream_of_its_own(q):
+    prefix, own = [100], [5, 40, 0]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ctx, keys, vals, x = case("bf16", 2, 128, 3, prefix, own, q)
+        out = torch.empty_like(x)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            B.sdsat_attention_shared(ctx.handle, 0, 3, q, 3, prefix, x, None, out)
+        g = torch.Generator(device="cuda")
+        g.manual_seed(3)
+        for _ in range(4):
+            x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+            out.fill_(7e7)
+            graph.replay()
+            s.synchronize()
+            replayed = out.clone()
+            ref, tol = reference(keys, vals, x, q, chain(keys, q))
+            check(replayed, ref, tol)
+            assert torch.equal(run(ctx, 3, prefix, q, x), replayed)
+    ctx.close()

@@ -1,0 +1,169 @@
+"""sdsat_kv_reorder against the same moves made on a host copy of the cache, bit for bit: forks, chains, cycles, freed
+sequences, ragged lengths, prefixes that stay, sequences outside the batch."""
+import random
+
+import pytest
+import torch
+
+from operator_helpers import context, device_error
+from paper_2403_18647_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def expected(k, v, lens, src, first):
+    """k, v on the host, [layers, B, heads, slots, ...] and [layers, B, heads, pages, ...]."""
+    k2, v2, l2 = k.clone(), v.clone(), list(lens)
+    for b, a in enumerate(src):
+        if a < 0:
+            l2[b] = 0
+            continue
+        l2[b] = lens[a]
+        lo, hi = first // 32, -(-lens[a] // 32)
+        if a != b and lo < hi:
+            k2[:, b, :, 32 * lo:32 * hi] = k[:, a, :, 32 * lo:32 * hi]
+            v2[:, b, :, lo:hi] = v[:, a, :, lo:hi]
+    return k2, v2, l2
+
+
+def fill(ctx, lens, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    k, v, length = ctx.cache()
+    k.copy_(torch.randn(k.shape, generator=g, device="cuda"))
+    v.copy_(torch.randn(v.shape, generator=g, device="cuda"))
+    B.sdsat_set_cache_len(ctx.handle, lens)
+    return k, v, length
+
+
+def check(ctx, lens, src, first, seed=1):
+    k, v, length = fill(ctx, lens, seed)
+    want = expected(k.cpu(), v.cpu(), lens, src, first)
+    B.sdsat_kv_reorder(ctx.handle, len(src), torch.tensor(src, dtype=torch.int32, device="cuda"), first)
+    torch.cuda.synchronize()
+    assert length.tolist() == want[2]
+    assert torch.equal(k.cpu(), want[0]) and torch.equal(v.cpu(), want[1])
+
+
+MAPS = {
+    "stays": [0, 1, 2, 3, 4, 5],
+    "fork": [0, 0, 0, 0, 0, 0],
+    "fork from the last": [5, 5, 5, 5, 5, 5],
+    "chain down": [1, 2, 3, 4, 5, 5],
+    "chain up": [0, 0, 1, 2, 3, 4],
+    "swap": [1, 0, 2, 3, 5, 4],
+    "cycle of six": [1, 2, 3, 4, 5, 0],
+    "cycle with branches": [1, 2, 0, 0, 1, 4],
+    "two cycles": [3, 4, 5, 0, 1, 2],
+    "freed": [-1, 0, -1, 3, 2, -1],
+    "freed cycle member's reader": [1, 0, -1, 2, 0, 0],
+    "all freed": [-1] * 6,
+    "compacted": [0, 5, 2, 4],
+    "one": [3],
+}
+
+
+@pytest.mark.parametrize("name", MAPS)
+@pytest.mark.parametrize("dtype,heads,dh", [("fp32", 3, 64), ("bf16", 2, 128)])
+def test_maps(name, dtype, heads, dh):
+    ctx = context(heads, dh, dtype, layers=2, batch=6, slots=150)
+    check(ctx, [70, 1, 32, 33, 0, 150], MAPS[name], 0)
+    check(ctx, [70, 129, 32, 64, 95, 0], MAPS[name], 64)
+    assert device_error(ctx) == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("first", [0, 1, 31, 32, 33, 96, 127, 128])
+@pytest.mark.parametrize("length", [0, 1, 31, 32, 33, 97, 128])
+def test_pages(first, length):
+    ctx = context(1, 64, "bf16", batch=3, slots=128)
+    check(ctx, [length, 128, 5], [1, 0, 0], first, seed=first + length)
+    ctx.close()
+
+
+def test_random_maps():
+    rng = random.Random(5)
+    ctx = context(1, 64, "bf16", batch=9, slots=96)
+    for i in range(40):
+        n = rng.randint(1, 9)
+        check(ctx, [rng.randint(0, 96) for _ in range(9)], [rng.randint(-1, 8) for _ in range(n)], rng.choice([0, 0, 40]), i)
+    assert device_error(ctx) == 0
+    ctx.close()
+
+
+def test_many_sequences():
+    """More sequences than a wave has lanes, a permutation with many cycles."""
+    rng = random.Random(6)
+    src = list(range(300))
+    rng.shuffle(src)
+    ctx = context(1, 64, "bf16", batch=300, slots=64)
+    check(ctx, [rng.randint(0, 64) for _ in range(300)], src, 0)
+    check(ctx, [rng.randint(0, 64) for _ in range(300)], [rng.randint(-1, 299) for _ in range(300)], 0)
+    ctx.close()
+
+
+def test_a_long_cache():
+    ctx = context(2, 128, "bf16", layers=3, batch=2, slots=40000)
+    check(ctx, [39990, 17], [1, 0], 0)
+    ctx.close()
+
+
+@pytest.mark.parametrize("bad", [-2, 4, 1 << 30])
+def test_a_source_out_of_range_is_reported_and_leaves_the_sequence(bad):
+    ctx = context(1, 64, "fp32", batch=4, slots=64)
+    k, v, length = fill(ctx, [10, 20, 30, 40], 3)
+    want = expected(k.cpu(), v.cpu(), [10, 20, 30, 40], [1, 1, 0, 3], 0)
+    B.sdsat_kv_reorder(ctx.handle, 4, torch.tensor([1, bad, 0, 3], dtype=torch.int32, device="cuda"), 0)
+    torch.cuda.synchronize()
+    assert length.tolist() == want[2] and torch.equal(k.cpu(), want[0]) and torch.equal(v.cpu(), want[1])
+    assert device_error(ctx) == -6
+    assert device_error(ctx) == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("batch,first,src,code", [(0, 0, True, -1), (5, 0, True, -1), (4, -1, True, -1), (4, 65, True, -1),
+                                                  (4, 0, False, -1)])
+def test_refusals(batch, first, src, code):
+    ctx = context(1, 64, "fp32", batch=4, slots=64)
+    with pytest.raises(B.SdsatError) as e:
+        B.sdsat_kv_reorder(ctx.handle, batch, torch.zeros(8, dtype=torch.int32, device="cuda") if src else None, first)
+    assert e.value.code == code
+    with pytest.raises(B.SdsatError) as e:
+        B.sdsat_cache_ptr(ctx.handle, 1)
+    assert e.value.code == -1
+    ctx.close()
+
+
+def test_cache_views_are_what_kv_write_wrote():
+    ctx = context(2, 64, "bf16", layers=2, batch=2, slots=70)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    k, v = (torch.randn((2, 70, 2, 64), generator=g, device="cuda") for _ in range(2))
+    B.sdsat_kv_write(ctx.handle, 1, 2, 70, k, v, torch.arange(70, dtype=torch.int32, device="cuda").repeat(2))
+    kc, vc, _ = ctx.cache()
+    torch.cuda.synchronize()
+    assert torch.equal(kc[1, :, :, :70], k.bfloat16().transpose(1, 2))
+    assert torch.equal(vc[1].reshape(2, 2, 96, 64)[:, :, :70], v.bfloat16().transpose(1, 2))
+    assert not kc[0].any() and not vc[0].any()
+    ctx.close()
+
+
+def test_captured_on_a_stream_of_its_own():
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ctx = context(2, 64, "bf16", layers=2, batch=4, slots=100)
+        src = torch.tensor([1, 2, 0, 1], dtype=torch.int32, device="cuda")
+        lens = [100, 40, 3, 77]
+        fill(ctx, lens, 1)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            B.sdsat_kv_reorder(ctx.handle, 4, src, 0)
+        for i in range(4):
+            k, v, length = fill(ctx, lens, 10 + i)
+            want = expected(k.cpu(), v.cpu(), lens, src.tolist(), 0)
+            graph.replay()
+            s.synchronize()
+            assert length.tolist() == want[2] and torch.equal(k.cpu(), want[0]) and torch.equal(v.cpu(), want[1])
+            check(ctx, lens, [3, 3, 1, 2], 32, seed=20 + i)   # the program's own calls between replays
+    ctx.close()
