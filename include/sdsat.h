@@ -182,7 +182,7 @@ int sdsat_verify_nucleus(sdsat_ctx* ctx, int32_t batch, int32_t q, const float* 
  *   d_top_ids, d_top_logprobs [batch*q, n_top]  the n_top most probable ids and
  *                       their log probabilities, the largest first, ties to the
  *                       lower id (NaN logits last).
- * n_top 0..32, at most V, V / 8192 * n_top <= 4096 (SDSAT_EUNSUPPORTED).
+ * n_top 0..32, at most V.
  * d_logprob (with d_tokens), d_entropy and, with n_top 0, the last two may be
  * NULL.  A row that holds NaN or whose largest logit is infinite (an empty row
  * of -inf among them) gives NaN log probabilities and entropy.  float32

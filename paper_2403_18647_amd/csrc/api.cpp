@@ -124,7 +124,7 @@ struct sdsat_ctx {
     float* shared_part = nullptr; // parts of shared-prefix attention
     size_t shared_part_floats = 0;
     int* reorder_steps = nullptr; // the copy list of a cache reordering
-    void* lp_part = nullptr;      // log probabilities: results of the chunks of a row, and (zero between launches) how
+    void* lp_part = nullptr;      // log probabilities: results of the segments of a row, and (zero between launches) how
     int* lp_ctr = nullptr;        // many have arrived
     int* cache_len = nullptr; int* err_flag = nullptr; int* verify_cnt = nullptr;
     unsigned long long* verify_best = nullptr;   // greedy verification: each row's best so far (zero between launches)
@@ -822,8 +822,6 @@ int sdsat_token_logprobs(sdsat_ctx* c, int32_t batch, int32_t q, const float* d_
         return fail(c, SDSAT_EINVAL, "temperature must be positive and finite");
     if (n_top < 0 || n_top > kMaxTop || n_top > c->D.V) return fail(c, SDSAT_EINVAL, "n_top must be 0..32 and at most V");
     if (n_top && (!d_top_ids || !d_top_logprobs)) return fail(c, SDSAT_EINVAL, "NULL top_ids or top_logprobs with n_top");
-    if ((long)logprob_chunks(c->D.V) * n_top > kMaxTopKeys)
-        return fail(c, SDSAT_EUNSUPPORTED, "n_top too large for this vocabulary (V / 8192 * n_top <= 4096)");
     if (!d_logprob && !d_entropy && !n_top) return SDSAT_OK;
     HIPCHK(c, launch_token_logprobs(d_logits, batch * q, c->D.V, d_tokens, temperature, n_top, d_logprob, d_entropy, d_top_ids,
                                     d_top_logprobs, c->lp_part, c->lp_ctr, c->err_flag, c->stream));

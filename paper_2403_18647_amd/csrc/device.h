@@ -152,4 +152,33 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
+// Reductions over lanes without LDS: neighbours by lane permutations within 16, then rows of 16 and halves of the wave
+// exchanged (gfx950).  Every lane gets the result; the order is fixed.
+template <int CTRL>
+__device__ __forceinline__ float lane_perm(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <typename F>
+__device__ __forceinline__ float across_rows(float v, F op) {   // lanes l, l ^ 16, l ^ 32, l ^ 48
+    const uint32_t u = __float_as_uint(v);
+    const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t t = __float_as_uint(op(__uint_as_float(p[0]), __uint_as_float(p[1])));
+    const auto r = __builtin_amdgcn_permlane32_swap(t, t, false, false);
+    return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <typename F>
+__device__ __forceinline__ float across_quads(float v, F op) {   // lanes 4k .. 4k + 3
+    v = op(v, lane_perm<0xB1>(v));
+    return op(v, lane_perm<0x4E>(v));
+}
+template <typename F>
+__device__ __forceinline__ float across_wave(float v, F op) {
+    v = across_quads(v, op);
+    v = op(v, lane_perm<0x141>(v));   // mirrored within 8 lanes, then 16
+    v = op(v, lane_perm<0x140>(v));
+    return across_rows(v, op);
+}
+struct OpMax { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct OpSum { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+
 }  // namespace sdsat

@@ -272,8 +272,6 @@ hipError_t launch_verify_nucleus(const float* logits, int B, int q, int V, const
 // Log probabilities of tokens (negative: none, 0 is written) under logits rows at a temperature, the rows' entropies
 // and n_top alternatives.  lp, ent: [M] or null; part: logprob_part_bytes; counter [M]: zero between launches
 constexpr int kMaxTop = 32;
-constexpr int kMaxTopKeys = 4096;      // chunks of a row times n_top, at most
-int logprob_chunks(int V);
 size_t logprob_part_bytes(int M, int V);
 hipError_t launch_token_logprobs(const float* logits, int M, int V, const int* tokens, float temperature, int n_top, float* lp,
                                  float* ent, int* ids, float* top_lp, void* part, int* counter, int* err, hipStream_t s);

@@ -10,16 +10,19 @@
 // differences; both terms of H are sums of positive numbers.  All sums are
 // float32 in a fixed order.
 //
-// A row is cut into chunks of 8192 ids, one workgroup each, which are read once
-// into registers (8 vector loads per thread in flight): the maximum, then the
-// sums, then the chunk's n_top largest.  For these, ids are held as 64-bit keys
-// (the logit as an order-preserving integer above the complement of the id), so
-// that every key differs and ties need no care.  64 groups of threads know
-// their largest keys; the n_top-th largest of those is at most the n_top-th
-// largest of the chunk, so only keys from it on are candidates (about 1.3
-// n_top for logits in no order); they are gathered in LDS and each is ranked
-// by counting the larger ones.  The chunk that arrives last joins the row's
-// results in chunk order.
+// A row is one segment, or several where there are few rows; one workgroup
+// streams each.  Its threads keep their own running maximum, sum and weighted
+// sum (no exchange while data arrives) and join them at the end.  For the n_top
+// largest, the lanes' running maxima serve: at least n_top of the wave's ids
+// reach the n_top-th largest of its 64 lanes' maxima, so only ids that do (and
+// exceed what earlier ids had set, ties going to the lower id) are candidates,
+// a few times n_top for logits in no order.  They are gathered in LDS as 64-bit
+// keys (the logit as an order-preserving integer above the complement of the
+// id: all differ, and ties need no care), thinned by the n_top-th largest of 64
+// groups of threads, and each is ranked by counting the larger ones.  Segments
+// with more candidates than LDS holds (many equal values, rising values) take
+// their ids one after the other.  The segment that arrives last joins the row's
+// results in segment order.
 #include <algorithm>
 
 #include "device.h"
@@ -27,12 +30,15 @@
 
 namespace sdsat {
 
-static constexpr int kLpNT = 256;
-static constexpr int kLpVec = 8;                              // vector loads per thread
-static constexpr int kLpChunk = kLpNT * 4 * kLpVec;           // ids per workgroup
-static constexpr int kLpGroups = 64;
-static constexpr int kLpMost = (kMaxTop - 1) * (kLpChunk / kLpGroups) + 1;   // candidates, at most
-static_assert(kMaxTop <= kLpGroups && kLpMost <= kMaxTopKeys, "one threshold key per group; candidates fit LDS");
+static constexpr int kLpNT = 256, kLpWaves = kLpNT / 64;
+static constexpr int kLpVec = 4;                              // vector loads per thread and tile
+static constexpr int kLpTile = 64 * 4 * kLpVec;               // ids a wave takes at a time
+static constexpr int kLpStep = kLpWaves * kLpTile;            // segments are multiples of it
+static constexpr int kLpCand = 384;                           // candidates of a wave, at most
+static constexpr int kLpFew = 384;                            // candidates of a segment that are ranked, at most
+static constexpr int kLpGrid = 1024;                          // rows are cut into as many segments together, at most
+static constexpr int kLpSegments = 64, kLpKeys = 1024;        // segments of a row, and their keys in the join, at most
+static_assert(kMaxTop <= 64 && kLpKeys <= kLpWaves * kLpCand, "lanes for the thresholds, LDS for the join");
 
 typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));   // logits rows are float-aligned
 typedef unsigned long long u64;
@@ -49,11 +55,7 @@ __device__ __forceinline__ float key_logit(uint32_t k) {
     return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k);
 }
 
-__device__ __forceinline__ u64 max64(u64 a, u64 b) { return a > b ? a : b; }
-
-__device__ __forceinline__ u64 shfl_xor64(u64 v, int o) {
-    return (u64)__shfl_xor((int)(v >> 32), o, 64) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)v, o, 64);
-}
+__device__ __forceinline__ u64 id_key(float f, int id) { return (u64)logit_key(f) << 32 | (uint32_t)~(uint32_t)id; }
 
 template <typename V>
 __device__ __forceinline__ void agent_store(V* p, V v) {
@@ -65,203 +67,375 @@ __device__ __forceinline__ V agent_load(const V* p) {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// The n largest of cand[0..count), in order, to out (agent-scope where another workgroup reads it)
-template <typename F>
-__device__ __forceinline__ void rank_candidates(const u64* cand, int count, int n, F out) {
-    for (int i = threadIdx.x; i < count; i += kLpNT) {
-        const u64 k = cand[i];
+__device__ __forceinline__ u64 pack2(float lo, float hi) { return (u64)__float_as_uint(hi) << 32 | __float_as_uint(lo); }
+
+// The n largest of cand[0..count), all different, in order to out[0..n): eight lanes count the keys above one
+__device__ __forceinline__ void rank_candidates(const u64* cand, int count, int n, u64* out) {
+    const int sub = threadIdx.x & 7;
+    for (int i0 = 0; i0 < count; i0 += kLpNT / 8) {   // every lane takes part in the sums
+        const int i = i0 + (threadIdx.x >> 3);
+        const u64 k = cand[min(i, count - 1)];
         int r = 0;
-        for (int j = 0; j < count; ++j) r += cand[j] > k;
-        if (r < n) out(r, k);
+        for (int j0 = 0; j0 < count; j0 += 32) {      // past the end the last is read again
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int j = j0 + 8 * u + sub;
+                r += j < count && cand[min(j, count - 1)] > k;
+            }
+        }
+        float f = across_quads((float)r, OpSum());
+        f += lane_perm<0x141>(f);
+        r = (int)f;
+        if (sub == 0 && i < count && r < n) out[r] = k;
     }
 }
 
+// A value that at least n of the wave's 64 reach: the n-th largest, to the 16 leading bits of its key.
+__device__ __forceinline__ float nth_largest(float v, int n) {
+    const uint32_t key = logit_key(v);
+    u64 in = ~0ull;   // lanes whose leading bits are those of the n-th largest
+    uint32_t got = 0;
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+        const u64 set = in & __ballot((key >> b) & 1u);
+        const int k = __popcll(set);
+        if (k >= n) {
+            in = set;
+            got |= 1u << b;
+        } else {
+            n -= k;
+            in &= ~set;
+        }
+    }
+    return got > 0x007FFFFFu ? key_logit(got) : -INFINITY;   // below the key of -inf: everything
+}
+
+// The running sums of a part of a row, with z in units of log 2: the maximum m, the sum of 2^(z - m) without one
+// largest term, and the sum of (z - m) 2^(z - m).
+struct LpSums { float m, s, w; };
+
+// a and b joined (z = x * scale); of equal maxima, a's term stays the one left out
+__device__ __forceinline__ LpSums lp_join(const LpSums& a, const LpSums& b, float scale) {
+    const float m = fmaxf(a.m, b.m);
+    const bool of_a = a.m >= b.m;
+    const float hi_s = of_a ? a.s : b.s, hi_w = of_a ? a.w : b.w, lo_m = of_a ? b.m : a.m;
+    const float lo_s = of_a ? b.s : a.s, lo_w = of_a ? b.w : a.w;
+    if (lo_m == -INFINITY) return {m, hi_s + lo_s, hi_w};   // no mass (NaN stays)
+    const float d = (lo_m - m) * scale, f = __builtin_amdgcn_exp2f(d);
+    return {m, hi_s + f * (1.f + lo_s), fmaf(f, fmaf(fmaxf(d, -1000.f), 1.f + lo_s, lo_w), hi_w)};   // 2^-1000 is 0
+}
+
+// The wave's sums joined; of equal maxima, the first lane's term stays the one left out.
+__device__ __forceinline__ LpSums lp_join_wave(const LpSums& v, float scale) {
+    const float m = across_wave(v.m, OpMax());
+    const u64 top = __ballot(v.m == m);
+    const float one = top && (int)(threadIdx.x & 63) == __builtin_ctzll(top) ? 0.f : 1.f;
+    const bool none = v.m == -INFINITY;   // no mass (NaN stays)
+    const float d = none ? 0.f : (v.m - m) * scale, f = __builtin_amdgcn_exp2f(d);
+    const float s = none ? v.s : f * (one + v.s), w = none ? 0.f : f * fmaf(fmaxf(d, -1000.f), 1.f + v.s, v.w);
+    return {m, across_wave(s, OpSum()), across_wave(w, OpSum())};
+}
+
 struct LogprobArgs {
-    const float* logits; int M, V, chunks;
+    const float* logits; int M, V, segs, seg;   // segments of a row, ids of each (the last takes the rest)
     const int* tokens; float inv_t; int n_top;
     float* lp; float* ent; int* ids; float* top_lp;
-    // [M][chunks]: the chunk's largest key, S without it and the weighted sum, then n_top keys
-    u64* part; int* counter;
+    u64* part; u64* keys;                       // [M][segs][2]: the sums; [M][segs][n_top]: the largest keys
+    int* counter;
+    int per, per_inv;                           // join: first keys of each segment behind the threshold; ceil(2^16 / per)
     int* err;
 };
 
-__global__ void __launch_bounds__(kLpNT) token_logprobs_kernel(LogprobArgs a) {
-    __shared__ u64 s_cand[kMaxTopKeys];
-    __shared__ u64 s_group[kLpGroups];
-    __shared__ u64 s_key[kLpNT / 64];
-    __shared__ float s_s[kLpNT / 64], s_w[kLpNT / 64];
-    __shared__ int s_count, s_last;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int row = (int)blockIdx.x / a.chunks, ch = (int)blockIdx.x % a.chunks, lo = ch * kLpChunk;
-    const int n = min(kLpChunk, a.V - lo);
+__global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a) {
+    __shared__ u64 s_cand[kLpWaves * kLpCand];
+    __shared__ u64 s_top[kMaxTop], s_key[kLpWaves];   // the largest keys, in order
+    __shared__ u64 s_few[kLpFew];
+    __shared__ float s_group[64];
+    __shared__ LpSums s_sums[kLpWaves];
+    __shared__ int s_count[kLpWaves], s_left, s_last;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int row = (int)blockIdx.x / a.segs, sg = (int)blockIdx.x % a.segs, lo = sg * a.seg;
+    const int n = min(a.seg, a.V - lo), n_top = a.n_top;
     const float* x = a.logits + (size_t)row * a.V + lo;
+    // the row's token and its logit, asked for now: only the row's last workgroup needs them
+    const int tok = a.lp ? a.tokens[row] : -1;
+    const float tok_x = tok >= 0 && tok < a.V ? a.logits[(size_t)row * a.V + tok] : 0.f;
+    if (tid == 0) s_left = 0;
+    if (lane == 0) s_count[wave] = 0;   // used by this wave alone while it streams
+    const float scale = a.inv_t * 1.44269504f;
 
-    float v[kLpVec][4];
+    // ids base + 256 i + 4 lane + j of the wave's tile at `base`; past the segment: -inf
+    auto load = [&](float (&v)[kLpVec][4], int base) {
+        if (base + kLpTile <= n) {
 #pragma unroll
-    for (int i = 0; i < kLpVec; ++i) {
-        const int id = (i * kLpNT + tid) * 4;
-        if (id + 4 <= n) {
-            const f32x4u_t t = *reinterpret_cast<const f32x4u_t*>(x + id);
+            for (int i = 0; i < kLpVec; ++i) {
+                const f32x4u_t t = *reinterpret_cast<const f32x4u_t*>(x + base + 256 * i + 4 * lane);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[i][j] = t[j];
+                for (int j = 0; j < 4; ++j) v[i][j] = t[j];
+            }
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[i][j] = id + j < n ? x[id + j] : -INFINITY;
+            for (int i = 0; i < kLpVec; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int id = base + 256 * i + 4 * lane + j;
+                    v[i][j] = id < n ? x[id] : -INFINITY;
+                }
         }
-    }
-    if (tid == 0) s_count = 0;
-    // this thread's largest key; ids past the row have none
-    auto key = [&](int i, int j) -> u64 {
-        const int id = (i * kLpNT + tid) * 4 + j;
-        return id < n ? (u64)logit_key(v[i][j]) << 32 | (uint32_t)~(uint32_t)(lo + id) : 0ull;
     };
-    u64 best = 0;
+    LpSums r{-INFINITY, 0.f, 0.f};
+    float ones = 0.f;                       // terms of 1 at the present maximum (none while it is -inf)
+    auto add = [&](const float (&v)[kLpVec][4]) {
+        float tm = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kLpVec; ++i)
+        for (int i = 0; i < kLpVec; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) best = max64(best, key(i, j));
-    u64 grp = max64(best, shfl_xor64(best, 1));   // groups of 4 threads
-    grp = max64(grp, shfl_xor64(grp, 2));
-    if ((tid & 3) == 0) s_group[tid >> 2] = grp;
-#pragma unroll
-    for (int o = 4; o < 64; o <<= 1) grp = max64(grp, shfl_xor64(grp, o));
-    if (lane == 0) s_key[wave] = grp;
-    __syncthreads();
-    u64 top = s_key[0];
-#pragma unroll
-    for (int w = 1; w < kLpNT / 64; ++w) top = max64(top, s_key[w]);
-    const float m = key_logit((uint32_t)(top >> 32));
-    const float base = m == -INFINITY || m != m ? 0.f : m;
-
-    // sums without the largest id's term
-    float s = 0.f, w = 0.f;
-#pragma unroll
-    for (int i = 0; i < kLpVec; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float t = (v[i][j] - base) * a.inv_t;
-            float e = __builtin_amdgcn_exp2f(t * 1.44269504f);
-            if (key(i, j) == top && e == e) e = 0.f;   // NaN stays
-            s += e;
-            w += e == 0.f ? 0.f : -t * e;              // t may be -inf there
+            for (int j = 0; j < 4; ++j) tm = fmaxf(tm, v[i][j]);
+        if (tm > r.m) {   // the sums so far relative to the new maximum, their largest terms ordinary ones now
+            const float d = fmaxf((r.m - tm) * scale, -1000.f), f = __builtin_amdgcn_exp2f(d);
+            r.w = f * fmaf(d, ones + r.s, r.w);
+            r.s = f * (ones + r.s);
+            r.m = tm;
+            ones = 0.f;
         }
-    s = wave_sum(s);
-    w = wave_sum(w);
-    if (lane == 0) { s_s[wave] = s; s_w[wave] = w; }
-
-    // the chunk's n_top largest keys, in order, at s_group[0..]
-    if (a.n_top > 0) {
-        u64 mine = s_group[lane];
-        int r = 0;
-        for (int j = 0; j < kLpGroups; ++j) r += s_group[j] > mine;
-        // groups past the row's end have key 0 and are tied at the end; the threshold is then 0 (every id)
-        const u64 at = __ballot(r == a.n_top - 1 && mine != 0);
-        const int src = at ? __builtin_ctzll(at) : 0;
-        const u64 thr = at ? s_group[src] : 1ull;
+        const float at = r.m == -INFINITY ? 0.f : r.m;
+        float all = 0.f, some = 0.f, w = 0.f;
 #pragma unroll
         for (int i = 0; i < kLpVec; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const u64 k = key(i, j);
-                if (k >= thr) s_cand[atomicAdd(&s_count, 1)] = k;
+                const float t = (v[i][j] - at) * scale, e = __builtin_amdgcn_exp2f(t);
+                all += e;
+                some += __builtin_amdgcn_fractf(e);   // 0 for the largest terms, which are 1
+                w = fmaf(fmaxf(t, -1000.f), e, w);    // -inf adds nothing
             }
-        __syncthreads();   // candidates complete; every wave has read the group keys
-        if (tid < kLpGroups) s_group[tid] = 0;
-        __syncthreads();
-        rank_candidates(s_cand, s_count, a.n_top, [&](int r, u64 k) { s_group[r] = k; });
+        ones += rintf(all - some);
+        r.s += some;
+        r.w += w;
+        return tm;
+    };
+    // the tile's ids that reach `least` become candidates
+    const bool one_step = n <= kLpStep;
+    u64* cand = one_step ? s_few : s_cand + wave * kLpCand;
+    int* counter = one_step ? &s_left : &s_count[wave];
+    const int room = one_step ? kLpFew : kLpCand;
+    auto push = [&](const float (&v)[kLpVec][4], int base, float tm, float least) {
+        if (tm < least) return;
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < kLpVec; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c += v[i][j] >= least;
+        int p = atomicAdd(counter, c);
+#pragma unroll
+        for (int i = 0; i < kLpVec; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (v[i][j] >= least) {
+                    if (p < room) cand[p] = id_key(v[i][j], lo + base + 256 * i + 4 * lane + j);
+                    ++p;
+                }
+    };
+    const float lowest = -3.402823466e38f;   // banned ids (-inf) are not taken
+    {
+        float v0[kLpVec][4], v1[kLpVec][4];
+        int base = wave * kLpTile;
+        load(v0, base);
+        if (base + kLpStep < n) load(v1, base + kLpStep);
+        const float tm = add(v0);
+        float reach = -INFINITY;   // n_top ids of earlier tiles reach it
+        if (n_top > 0) {
+            // the first tiles of all waves: 64 groups of 4 threads
+            const float gm = across_quads(r.m, OpMax());
+            if ((lane & 3) == 0) s_group[tid >> 2] = gm;
+            __syncthreads();
+            reach = nth_largest(s_group[lane], n_top);
+            push(v0, base, tm, fmaxf(reach, lowest));
+        }
+        // later ids that only tie with what earlier ones reach lose
+        int k = 1;
+        auto later = [&](const float (&v)[kLpVec][4], int b) {
+            const float t = add(v);
+            if (n_top == 0) return;
+            float least = fmaxf(key_logit(logit_key(reach) + 1), lowest);
+            if ((k & 7) == 7 && (k & (k + 1)) == 0) {   // tiles 7, 15, 31, ..: the wave alone has seen more than the first tiles held
+                const float now = nth_largest(r.m, n_top);
+                if (now > reach) least = reach = now;
+            }
+            push(v, b, t, least);
+            ++k;
+        };
+        base += kLpStep;
+        while (base < n) {
+            const int next = base + kLpStep, after = next + kLpStep;
+            if (next < n) load(v0, next);
+            later(v1, base);
+            if (next >= n) break;
+            if (after < n) load(v1, after);
+            later(v0, next);
+            base = after;
+        }
+    }
+    if (ones > 1.f) r.s += ones - 1.f;   // one of the largest terms stays out
+
+    // The largest keys of xs[0..len) (ids from id0), one after the other: for more candidates than LDS holds, and for
+    // rows with fewer finite logits than n_top.
+    auto one_by_one = [&](const float* xs, int len, int id0) {
+        u64 last = ~0ull, best = 0;
+        for (int k = 0; k < min(n_top, len); ++k) {
+            if (k == 0 || best == last) {   // this thread's was taken: its next one
+                best = 0;
+                for (int id = tid; id < len; id += kLpNT) {
+                    const u64 key = id_key(xs[id], id0 + id);
+                    if (key < last && key > best) best = key;
+                }
+            }
+            u64 top = best;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                const u64 other = (u64)(uint32_t)__shfl_xor((int)(top >> 32), o, 64) << 32 |
+                                  (uint32_t)__shfl_xor((int)(uint32_t)top, o, 64);
+                if (other > top) top = other;
+            }
+            __syncthreads();   // the round before has read s_key
+            if (lane == 0) s_key[wave] = top;
+            __syncthreads();
+            last = s_key[0];
+#pragma unroll
+            for (int o = 1; o < kLpWaves; ++o) if (s_key[o] > last) last = s_key[o];
+            if (tid == 0) s_top[k] = last;
+        }
+    };
+
+    // the segment's sums and its n_top largest keys (of finite logits, if it is one of several), in order, in s_top
+    {
+        const LpSums u = lp_join_wave(r, scale);
+        if (lane == 0) s_sums[wave] = u;
+    }
+    if (tid < kMaxTop) s_top[tid] = 0;
+    if (n_top > 0 && !one_step) {   // of the waves' candidates, those that reach the n_top-th largest of 64 groups
+        const float gm = across_quads(r.m, OpMax());
+        __syncthreads();   // the first thresholds have been read
+        if ((lane & 3) == 0) s_group[tid >> 2] = gm;
     }
     __syncthreads();
-    s = s_s[0]; w = s_w[0];
+    r = s_sums[0];
 #pragma unroll
-    for (int k = 1; k < kLpNT / 64; ++k) { s += s_s[k]; w += s_w[k]; }
-
-    const int stride = 2 + a.n_top;
-    u64* part = a.part + (size_t)row * a.chunks * stride;
-    if (a.chunks > 1) {
-        // the chunk's results, stored device-coherent: the row's last chunk may run on another XCD
-        u64* mine = part + (size_t)ch * stride;
-        if (tid == 0) {
-            agent_store(mine, top);
-            agent_store(mine + 1, (u64)__float_as_uint(w) << 32 | __float_as_uint(s));
+    for (int k = 1; k < kLpWaves; ++k) r = lp_join(r, s_sums[k], scale);
+    if (n_top > 0) {
+        int most = 0;
+        if (!one_step) {
+#pragma unroll
+            for (int k = 0; k < kLpWaves; ++k) most = max(most, s_count[k]);
+            if (most <= kLpCand) {
+                const uint32_t least = logit_key(nth_largest(s_group[lane], n_top));
+                for (int i = lane; i < s_count[wave]; i += 64) {
+                    const u64 k = cand[i];
+                    if ((uint32_t)(k >> 32) >= least) {
+                        const int p = atomicAdd(&s_left, 1);
+                        if (p < kLpFew) s_few[p] = k;
+                    }
+                }
+            }
+            __syncthreads();
         }
-        if (tid < a.n_top) agent_store(mine + 2 + tid, s_group[tid]);
-        __builtin_amdgcn_s_waitcnt(0);   // performed before the count is raised
+        const int left = s_left;
+        if (most <= kLpCand && left <= kLpFew && (left >= n_top || a.segs > 1)) rank_candidates(s_few, left, n_top, s_top);
+        else one_by_one(x, n, lo);
         __syncthreads();
+    }
+
+    if (a.segs > 1) {
+        u64* part = a.part + (size_t)row * a.segs * 2;
+        u64* keys = a.keys + (size_t)row * a.segs * n_top;
+        // the segment's results, stored device-coherent: the row's last segment may run on another XCD
         if (tid == 0) {
-            s_last = __hip_atomic_fetch_add(&a.counter[row], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.chunks - 1;
+            agent_store(part + 2 * sg, pack2(r.m, r.s));
+            agent_store(part + 2 * sg + 1, pack2(r.w, 0.f));
+        }
+        if (tid < n_top) agent_store(keys + sg * n_top + tid, s_top[tid]);
+        __builtin_amdgcn_s_waitcnt(0);   // performed before the count is raised (wave 0 stored everything)
+        if (tid == 0) {
+            s_last = __hip_atomic_fetch_add(&a.counter[row], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.segs - 1;
             if (s_last) agent_store(&a.counter[row], 0);
+            s_left = 0;
         }
         __syncthreads();
         if (!s_last) return;
-        // join: the largest key, then each chunk's sums relative to it, in chunk order
-        for (int c = 0; c < a.chunks; ++c) top = max64(top, agent_load(part + (size_t)c * stride));
-        const float mm = key_logit((uint32_t)(top >> 32));
-        s = w = 0.f;
-        for (int c = 0; c < a.chunks; ++c) {
-            const u64 k = agent_load(part + (size_t)c * stride), sw = agent_load(part + (size_t)c * stride + 1);
-            const float cs = __uint_as_float((uint32_t)sw), cw = __uint_as_float((uint32_t)(sw >> 32));
-            const float cm = key_logit((uint32_t)(k >> 32));
-            if (k == top) {
-                s += cs;
-                w += cw;
-            } else if (cm == -INFINITY || cm != cm) {   // a chunk of banned ids has no mass (NaN stays)
-                s += cs;
-            } else {
-                const float d = (cm - mm) * a.inv_t, f = __builtin_amdgcn_exp2f(d * 1.44269504f);
-                s += f * (1.f + cs);
-                w += f == 0.f ? f * cs : f * (cw - d * (1.f + cs));   // d may be -inf there
-            }
+        // join: a segment per lane; of the keys, if they are many, those that reach a threshold from the first keys of each
+        // segment.  Everything is asked for at once
+        const int n_keys = a.segs * n_top;
+        const bool thin = n_keys > 96;
+        u64 key[kLpKeys / kLpNT], first = 0;
+#pragma unroll
+        for (int i = 0; i < kLpKeys / kLpNT; ++i)
+            key[i] = tid + i * kLpNT < n_keys ? agent_load(keys + tid + i * kLpNT) : 0;
+        if (thin) {
+            const int c = (int)((uint32_t)(lane * a.per_inv) >> 16);   // lane / per
+            if (c < a.segs) first = agent_load(keys + c * n_top + lane - c * a.per);
         }
-        if (a.n_top > 0) {
-            // each chunk's keys are in order: a candidate's rank is its place there plus the larger keys of the others
-            for (int i = tid; i < a.chunks * a.n_top; i += kLpNT)
-                s_cand[i] = agent_load(part + (size_t)(i / a.n_top) * stride + 2 + i % a.n_top);
+        const u64 ms = lane < a.segs ? agent_load(part + 2 * lane) : pack2(-INFINITY, 0.f);
+        const u64 ww = lane < a.segs ? agent_load(part + 2 * lane + 1) : 0;
+        if (n_top > 0) {
+            // an empty place (a segment of fewer ids) is below every logit
+            const uint32_t least =
+                thin ? logit_key(nth_largest(first ? key_logit((uint32_t)(first >> 32)) : -INFINITY, n_top)) : 0;
+#pragma unroll
+            for (int i = 0; i < kLpKeys / kLpNT; ++i)
+                if (key[i] && (uint32_t)(key[i] >> 32) >= least) s_cand[atomicAdd(&s_left, 1)] = key[i];
             __syncthreads();
-            rank_candidates(s_cand, a.chunks * a.n_top, a.n_top, [&](int r, u64 k) { s_group[r] = k; });
-            __syncthreads();
+            if (s_left >= n_top) rank_candidates(s_cand, s_left, n_top, s_top);
+            else one_by_one(a.logits + (size_t)row * a.V, a.V, 0);
         }
+        r = lp_join_wave({__uint_as_float((uint32_t)ms), __uint_as_float((uint32_t)(ms >> 32)), __uint_as_float((uint32_t)ww)}, scale);
+        if (n_top > 0) __syncthreads();
     }
     // the row's results; without a finite largest logit they are NaN
-    const float mm = key_logit((uint32_t)(top >> 32));
-    const float log_s = log1pf(s);
+    const float log_s = log1pf(r.s);
     if (tid == 0) {
-        if (a.ent) a.ent[row] = isfinite(mm) ? log_s + w / (1.f + s) : NAN;
+        if (a.ent) a.ent[row] = isfinite(r.m) ? log_s - r.w * 0.693147181f / (1.f + r.s) : NAN;
         if (a.lp) {
-            const int t = a.tokens[row];
-            float r = 0.f;   // no token in this row
-            if (t >= a.V) {
+            float y = 0.f;   // no token in this row
+            if (tok >= a.V) {
                 atomicOr(a.err, 1);
-                r = NAN;
-            } else if (t >= 0) {
-                r = isfinite(mm) ? (a.logits[(size_t)row * a.V + t] - mm) * a.inv_t - log_s : NAN;
+                y = NAN;
+            } else if (tok >= 0) {
+                y = isfinite(r.m) ? (tok_x - r.m) * a.inv_t - log_s : NAN;
             }
-            a.lp[row] = r;
+            a.lp[row] = y;
         }
     }
-    if (tid < a.n_top) {
-        const u64 k = s_group[tid];
-        a.ids[(size_t)row * a.n_top + tid] = (int)~(uint32_t)k;
-        a.top_lp[(size_t)row * a.n_top + tid] =
-            isfinite(mm) ? (key_logit((uint32_t)(k >> 32)) - mm) * a.inv_t - log_s : NAN;
+    if (tid < n_top) {
+        const u64 k = s_top[tid];
+        a.ids[(size_t)row * n_top + tid] = (int)~(uint32_t)k;
+        a.top_lp[(size_t)row * n_top + tid] =
+            isfinite(r.m) ? (key_logit((uint32_t)(k >> 32)) - r.m) * a.inv_t - log_s : NAN;
     }
 }
 
-int logprob_chunks(int V) { return (V + kLpChunk - 1) / kLpChunk; }
-
-size_t logprob_part_bytes(int M, int V) {
-    const int c = logprob_chunks(V);
-    return c > 1 ? (size_t)M * c * (2 + kMaxTop) * 8 : 0;
+// Ids per segment: the fewest steps for which all segments run at a time (or each row is one), within what a join takes.
+static int logprob_segment(int M, int V, int n_top) {
+    const long steps = (V + kLpStep - 1) / kLpStep;
+    const long most = std::min<long>(kLpSegments, n_top > 0 ? kLpKeys / n_top : kLpSegments);
+    const long segs = std::max<long>(1, std::min<long>({steps, most, kLpGrid / M}));
+    return (int)std::min<long>((steps + segs - 1) / segs * kLpStep, 0x7FFFF000);
 }
+
+// Rows are cut while kLpGrid segments hold them all.
+size_t logprob_part_bytes(int M, int V) { return V > kLpStep ? (size_t)std::min<long>((long)M * kLpSegments, kLpGrid) * (2 + kMaxTop) * 8 : 0; }
 
 hipError_t launch_token_logprobs(const float* logits, int M, int V, const int* tokens, float temperature, int n_top, float* lp,
                                  float* ent, int* ids, float* top_lp, void* part, int* counter, int* err, hipStream_t s) {
-    const int chunks = logprob_chunks(V);
     if (M < 1 || V < 1 || !(temperature > 0.f) || n_top < 0 || n_top > kMaxTop || n_top > V || (lp && !tokens) ||
-        (n_top && (!ids || !top_lp)) || (chunks > 1 && (!part || !counter)) || (long)chunks * n_top > kMaxTopKeys)
+        (n_top && (!ids || !top_lp)))
         return hipErrorInvalidValue;
-    LogprobArgs a{logits, M, V, chunks, tokens, 1.0f / temperature, n_top, lp, ent, ids, top_lp, static_cast<u64*>(part), counter,
-                  err};
-    hipLaunchKernelGGL(token_logprobs_kernel, dim3((unsigned)((size_t)M * chunks)), dim3(kLpNT), 0, s, a);
+    const int seg = logprob_segment(M, V, n_top), segs = (int)(((long)V + seg - 1) / seg);
+    if (segs > 1 && (!part || !counter)) return hipErrorInvalidValue;
+    const int per = n_top > 0 ? std::min(n_top, 64 / segs) : 1;
+    u64* sums = static_cast<u64*>(part);
+    LogprobArgs a{logits, M, V, segs, seg, tokens, 1.0f / temperature, n_top, lp, ent, ids, top_lp,
+                  sums, sums + (size_t)2 * M * segs, counter, per, (65536 + per - 1) / per, err};
+    hipLaunchKernelGGL(token_logprobs_kernel, dim3((unsigned)((size_t)M * segs)), dim3(kLpNT), 0, s, a);
     return hipGetLastError();
 }
 
