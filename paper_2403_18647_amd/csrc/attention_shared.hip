@@ -10,20 +10,26 @@
 // (0..r, or the rows set in its ancestor mask).
 //
 // The softmax is cut into parts, each with its own maximum and sum:
-//  * a prefix part: rows of all sequences of a group (n * q rows, RT 16-row
-//    tiles per workgroup) against a range of shared pages, which are so read
-//    once for the group instead of once per sequence; no mask;
-//  * an own part: the q rows of one sequence against a range of its own pages.
-// A second kernel joins a row's parts (prefix parts in page order, then own
-// parts) by log-sum-exp.  Blocks of more than kAttnSplitRows rows have
-// workgroups enough and take both phases in one workgroup per 64 rows (WHOLE),
-// which writes the result itself.
+//  * prefix parts: rows of all sequences of a group (n * q rows) against a
+//    range of shared pages, which are so read once for the group instead of
+//    once per sequence; no mask;
+//  * own parts: the q rows of one sequence against a range of its own pages.
+// A second kernel joins a row's parts, prefix parts in page order, then own
+// parts, by log-sum-exp.  Blocks of more than kAttnSplitRows rows have workgroups
+// enough and take both phases in one workgroup per row tile, which writes the
+// result.
 //
-// Within a workgroup the 4 waves take the range's 32-key blocks round-robin;
-// each forms the scores of its block for all row tiles with K straight from the
-// cache as matrix-core fragments (S^T = K Q^T; Q in LDS), the softmax in
-// registers (rows in lanes, keys in registers and lane groups), and O^T += V^T
-// P^T with P as it stands; the next block's K and V are in flight meanwhile.
+// A part's 32-key blocks go round-robin over key lanes (2 for a prefix, 4 for
+// own slots), waves that keep their own maximum, sum and O, joined in lane order
+// at the end.  Scores are formed as S^T = K Q^T, the softmax runs in registers
+// (rows in lanes, keys in registers and lane groups), and O^T += V^T P^T takes P
+// as it stands.  Two kinds of workgroup do this, with the same values:
+//  * few rows, and float models: a wave per key lane and 16 rows, K and V
+//    straight from the cache into registers, the next block's in flight and its
+//    scores formed beside the present one's softmax; bound by HBM;
+//  * many rows of bf16 models: 64 rows, two key lanes of two waves with 32 rows
+//    each; the blocks go straight into LDS while the ones before are used, Q
+//    stays in registers; bound by the matrix cores.
 // On bf16 models Q and P enter the matrix cores as value and remainder, so that
 // float accuracy is kept.  Scores are in units of log 2 (the scale is folded
 // into Q) and a row's maximum is only raised when a score exceeds it by more
@@ -41,8 +47,9 @@
 
 namespace sdsat {
 
-static constexpr int kShareWaves = 4;
 static constexpr float kRaise = 8.f;
+static constexpr int kPrefixLanes = 2, kOwnLanes = 4;   // key lanes
+static constexpr int kTileRows = 64;                    // rows of a workgroup that stages K and V in LDS
 
 SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pages, int max_len, int S_max) {
     SharedPlan p{};
@@ -53,30 +60,30 @@ SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pag
         least = std::min(least, pages[g]);
     }
     p.whole = q > kAttnSplitRows;
-    // 16-row tiles per workgroup: float models keep one (registers); bf16 as many as a group's rows fill, up to 4
     const int rows = p.whole ? q : group * q;
-    p.rt = dtype == 0 ? 1 : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int tile = 16 * p.rt;
+    p.staged = dtype == 1 && rows > kSharedFewRows;
+    const int tile = p.staged ? kTileRows : 16;
+    p.tiles = (rows + tile - 1) / tile;
     if (p.whole) {
-        p.grid = B * H * ((q + tile - 1) / tile);
-        p.slots = 0;
+        p.grid = B * H * p.tiles;
         return p;
     }
-    // pages per prefix part: one for each wave at the least, and parts enough for kSharedParts workgroups
-    const int parts = std::min(kSharedMaxParts, std::max(1, (kSharedParts + G * H - 1) / (G * H)));
-    p.chunk = std::max(kShareWaves, (most + parts - 1) / parts);
+    // pages per prefix part: two for each lane at the least, and parts enough for kSharedParts workgroups
+    const int parts = std::min(kSharedMaxParts, std::max(1, kSharedParts / (G * H)));
+    p.chunk = std::max(2 * kPrefixLanes, (most + parts - 1) / parts);
     p.prefix_parts = (most + p.chunk - 1) / p.chunk;
-    // pages per own part: the own slots of a full cache in as many parts as fit kSharedParts workgroups
+    // pages per own part: the own slots of a full cache in as many parts as fit kSharedParts workgroups, 1024 slots at the
+    // least
     const int cap = S_max / 32 - least;
     const int own = std::min(kSharedMaxOwn, std::max(1, kSharedParts / (B * H)));
-    p.own_chunk = std::max(kShareWaves, (cap + own - 1) / own);
+    p.own_chunk = std::max(32, (cap + own - 1) / own);
     const int nblk = std::max(1, std::min(cap, (max_len + q + 31) / 32 - least));
     p.own_parts = (nblk + p.own_chunk - 1) / p.own_chunk;
     p.slots = p.prefix_parts + p.own_parts;
-    p.tiles = (rows + tile - 1) / tile;
-    p.own_tiles = (q + tile - 1) / tile;
-    p.prefix_grid = ((G * H * p.prefix_parts + 7) / 8 * 8) * p.tiles;
-    p.grid = p.prefix_grid + B * H * p.own_tiles * p.own_parts;
+    // workgroups of the prefix: one per part and row tile, of 64 rows or two of 16; then those of the own parts
+    const int units = (G * H * p.prefix_parts + 7) / 8 * 8 * p.tiles;
+    p.prefix_grid = p.staged ? units : (units + 15) / 16 * 8;
+    p.grid = p.prefix_grid + B * H * ((q + 15) / 16) * p.own_parts;
     return p;
 }
 
@@ -87,7 +94,7 @@ size_t shared_partial_floats(const SharedPlan& p, int B, int q, int H, int head_
 // The most any call can need: every row of a decode block, both kinds of part at their most.
 size_t shared_partial_floats_most(int B_max, int H, int q_max, int head_dim) {
     if (B_max < 2) return 0;   // a group of one takes the plain attention
-    const int parts = std::min(kSharedMaxParts, std::max(1, (kSharedParts + H - 1) / H));
+    const int parts = std::min(kSharedMaxParts, std::max(1, kSharedParts / H));
     size_t most = 0;
     for (int B = 2; B <= B_max; ++B) {
         const int own = std::min(kSharedMaxOwn, std::max(1, kSharedParts / (B * H)));
@@ -119,309 +126,556 @@ __device__ __forceinline__ void drop_keys(Frag<T>& f, int key0, int g, int Tb) {
 // What a block's rows may see: keys below L all, keys below Tb by the causal order or the ancestor masks.
 struct Sight { int L, Tb, q; const uint64_t* mask; };
 
-// One 32-key block for up to RT 16-row tiles (nt of them in use).  Row tile t's column c is block row m0 + 16 t + c;
-// only blocks with keys from L on look at it.
-template <typename T, int NDS, int NDT, int RT>
-__device__ __forceinline__ void attend(const Frag<T> (&kf)[2][NDS], Frag<T> (&vf)[NDT], const Frag<T>* qs, int lane, int nt,
-                                       int m0, const Sight& see, int blk, float (&rmax)[RT], float (&rsum)[RT],
-                                       f32x4_t (&o)[RT][NDT]) {
-    constexpr bool two = sizeof(T) == 2;
-    const int c = lane & 15, g = lane >> 4;
-    const bool whole = 32 * blk + 32 <= see.L;
-    if (32 * blk + 32 > see.Tb) {
+// One wave's share of an attention over 32-key blocks: RT 16-row tiles of queries, the scores of the block at hand, and
+// the running maxima, sums and weighted V of each row (row tile t's column c is row 16 t + c).
+template <typename T, int DH, int RT>
+struct WaveAttention {
+    static constexpr int NDT = DH / 16;
+    f32x4_t s[RT][2], o[RT][NDT];   // s[t][kt][r] = S^T[key 16 kt + 4 g + r][row 16 t + c]
+    float rmax[RT], rsum[RT];
+
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) drop_keys<T>(vf[dt], 32 * blk, g, see.Tb);
+        for (int t = 0; t < RT; ++t) {
+            rmax[t] = -INFINITY;
+            rsum[t] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) o[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
     }
+    // The scores of block blk as its rows see them, and the maxima raised where they have to be.  m0: block row of tile 0.
+    __device__ __forceinline__ void look(int blk, int m0, const Sight& see, int lane) {
+        const int c = lane & 15, g = lane >> 4;
+        if (32 * blk + 32 > see.L) {
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        if (t >= nt) break;
-        f32x4_t s0 = f32x4_t{0.f, 0.f, 0.f, 0.f}, s1 = s0;
+            for (int t = 0; t < RT; ++t) {
+                const int m = m0 + 16 * t + c;
+                const uint64_t mrow = see.mask && m < see.q ? see.mask[m] : 0ull;
 #pragma unroll
-        for (int ds = 0; ds < NDS; ++ds) {
-            constexpr int P = two ? 2 : 1;
-            const Frag<T> qh = lds_frag<T>(qs, (t * P * NDS + ds) * 64 + lane);
-            mma(s0, kf[0][ds], qh);
-            mma(s1, kf[1][ds], qh);
-            if constexpr (two) {
-                const Frag<T> ql = lds_frag<T>(qs, (t * P * NDS + NDS + ds) * 64 + lane);
-                mma(s0, kf[0][ds], ql);
-                mma(s1, kf[1][ds], ql);
+                for (int e = 0; e < 8; ++e) {
+                    const int key = 32 * blk + 16 * (e / 4) + 4 * g + e % 4;
+                    bool v = key < see.Tb && m < see.q;
+                    if (see.mask) v = v && (key < see.L || ((mrow >> (key - see.L)) & 1ull));
+                    else v = v && key <= see.L + m;
+                    if (!v) s[t][e / 4][e % 4] = -INFINITY;
+                }
             }
         }
-        float sv[8];
+        float lm[RT];
+        bool rise = false;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sv[e] = e < 4 ? s0[e] : s1[e - 4];
-        if (!whole) {
-            const int m = m0 + 16 * t + c;
-            const uint64_t mrow = see.mask && m < see.q ? see.mask[m] : 0ull;
+        for (int t = 0; t < RT; ++t) {
+            lm[t] = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])),
+                          fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
+            rise |= lm[t] > rmax[t] + kRaise;
+        }
+        if (__any(rise)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int key = 32 * blk + 16 * (e / 4) + 4 * g + e % 4;
-                bool v = key < see.Tb && m < see.q;
-                if (see.mask) v = v && (key < see.L || ((mrow >> (key - see.L)) & 1ull));
-                else v = v && key <= see.L + m;
-                if (!v) sv[e] = -INFINITY;
+            for (int t = 0; t < RT; ++t) {
+                const float bm = across_rows(lm[t], OpMax());
+                if (bm > rmax[t] + kRaise) {   // rows whose maximum stays are left as they are
+                    const float alpha = __builtin_amdgcn_exp2f(rmax[t] - bm);
+                    rmax[t] = bm;
+                    rsum[t] *= alpha;
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt) o[t][dt] *= alpha;
+                }
             }
         }
-        const float lm = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])),
-                               fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
-        if (__any(lm > rmax[t] + kRaise)) {
-            float bm = fmaxf(lm, __shfl_xor(lm, 16, 64));
-            bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
-            if (bm > rmax[t] + kRaise) {   // rows whose maximum stays are left as they are
-                const float alpha = __builtin_amdgcn_exp2f(rmax[t] - bm);
-                rmax[t] = bm;
-                rsum[t] *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < NDT; ++dt) o[t][dt] *= alpha;
-            }
-        }
+    }
+    // The weights of tile t's scores as matrix operands, and their sum.
+    __device__ __forceinline__ void weigh(int t, Frag<T>& ph, Frag<T>& pl) {
         const float base = rmax[t] == -INFINITY ? 0.f : rmax[t];   // a row that has seen no key yet
-        float p[8];
-        float ps = 0.f;
+        float p[8], ps = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(sv[e] - base);
+            p[e] = __builtin_amdgcn_exp2f(s[t][e / 4][e % 4] - base);
             ps += p[e];
         }
         rsum[t] += ps;
-        Frag<T> ph, pl;
         split_frag<T>(p, ph, pl);
+    }
+};
+
+// acc += a * (hi + lo)
+template <typename T>
+__device__ __forceinline__ void mma2(f32x4_t& acc, const Frag<T>& a, const Frag<T>& hi, const Frag<T>& lo) {
+    mma(acc, a, hi);
+    if constexpr (sizeof(T) == 2) mma(acc, a, lo);
+}
+
+// The cache rows of a head that an attention reads: pages below `pages` from the group's first sequence, the others from
+// the sequence itself.
+template <typename T>
+struct HeadCache {
+    const T *k0, *v0, *k1, *v1;
+    int pages;
+};
+template <typename T, int DH>
+__device__ __forceinline__ HeadCache<T> head_cache(const AttnArgs& at, int first, int own, int h, int pages) {
+    const size_t o0 = ((size_t)first * at.H + h) * at.S_max * DH, o1 = ((size_t)own * at.H + h) * at.S_max * DH;
+    const T* kc = reinterpret_cast<const T*>(at.kc);
+    const T* vc = reinterpret_cast<const T*>(at.vc);
+    return {kc + o0, vc + o0, kc + o1, vc + o1, pages};
+}
+
+// Eight query columns scaled into units of log 2, as value and remainder.
+template <typename T>
+__device__ __forceinline__ void query_frag(const AttnArgs& at, const float* q8, Frag<T>& hi, Frag<T>& lo) {
+    const f32x4u_t a = reinterpret_cast<const f32x4u_t*>(q8)[0], b = reinterpret_cast<const f32x4u_t*>(q8)[1];
+    const float x[8] = {a.x * at.scale, a.y * at.scale, a.z * at.scale, a.w * at.scale,
+                        b.x * at.scale, b.y * at.scale, b.z * at.scale, b.w * at.scale};
+    split_frag<T>(x, hi, lo);
+}
+
+// ------------------------------------------------------------------ 16 rows, K and V from the cache to registers
+// The attention of rows row0 .. row0 + rows - 1 (at most 16) over blocks from lo, a wave per key lane (`wave` of LANES).
+// The first blocks are requested (below hi) before the queries and before late(hi) says what the rows see and where the
+// blocks end; a block past the wave's last is asked for past the end of the buffer, which reads no memory.
+template <typename T, int DH, int LANES, typename F>
+__device__ __forceinline__ void attend_few(WaveAttention<T, DH, 1>& w, const AttnArgs& at, const HeadCache<T>& hc, int lo, int hi,
+                                           int row0, int rows, int h, int m0, int wave, int lane, F late) {
+    constexpr int NDS = DH / 32, NDT = DH / 16;
+    constexpr uint32_t E = sizeof(T);
+    constexpr bool ahead = E == 2 || DH == 64;   // float heads of 128: the registers hold one block's V
+    const int c = lane & 15, g = lane >> 4, none = at.S_max / 32;
+    const uint32_t bytes = (uint32_t)at.S_max * DH * E;
+    const __amdgpu_buffer_rsrc_t k0 = buf_rsrc(hc.k0, bytes), v0 = buf_rsrc(hc.v0, bytes), k1 = buf_rsrc(hc.k1, bytes),
+                                 v1 = buf_rsrc(hc.v1, bytes);
+    auto get_k = [&](Frag<T> (&kf)[2][NDS], int j) {
+        const __amdgpu_buffer_rsrc_t r = j < hc.pages ? k0 : k1;
+        const int blk = j < hi ? j : none;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const uint32_t ko = ((uint32_t)(blk * 32 + 16 * kt + c) * DH + 8 * g) * E;
+#pragma unroll
+            for (int ds = 0; ds < NDS; ++ds) kf[kt][ds] = buf_frag<T>(r, ko, ds * 32 * E);
+        }
+    };
+    auto get_v = [&](Frag<T> (&vf)[NDT], int j) {
+        const __amdgpu_buffer_rsrc_t r = j < hc.pages ? v0 : v1;
+        const uint32_t vo = ((uint32_t)(j < hi ? j : none) * DH * 32 + c * 32 + 8 * g) * E;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) vf[dt] = buf_frag<T>(r, vo, dt * 16 * 32 * E);
+    };
+    Frag<T> kA[2][NDS], kB[2][NDS], vA[NDT], qh[NDS], ql[NDS];
+    int i = lo + wave;
+    get_k(kA, i);
+    if constexpr (ahead) get_v(vA, i);
+    get_k(kB, i + LANES);
+    {
+        const float* q0 = at.qbuf + ((size_t)(row0 + min(c, rows - 1)) * at.H + h) * DH + 8 * g;   // rows past the last repeat it
+#pragma unroll
+        for (int ds = 0; ds < NDS; ++ds) query_frag<T>(at, q0 + 32 * ds, qh[ds], ql[ds]);
+    }
+    w.clear();
+    const Sight see = late(hi);
+    auto score = [&](const Frag<T> (&kf)[2][NDS]) {
+        w.s[0][0] = w.s[0][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ds = 0; ds < NDS; ++ds) {
+            mma2(w.s[0][0], kf[0][ds], qh[ds], ql[ds]);
+            mma2(w.s[0][1], kf[1][ds], qh[ds], ql[ds]);
+        }
+    };
+    // block i, its scores formed: K of the next block in kn, V in v
+    auto use = [&](const Frag<T> (&kn)[2][NDS], Frag<T> (&v)[NDT]) {
+        w.look(i, m0, see, lane);
+        if (32 * i + 32 > see.Tb) {   // keys that no row sees: their V may be anything
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) drop_keys<T>(v[dt], 32 * i, g, see.Tb);
+        }
+        Frag<T> ph, pl;
+        w.weigh(0, ph, pl);
+        score(kn);
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) mma2(w.o[0][dt], v[dt], ph, pl);
+    };
+    score(kA);
+    if constexpr (ahead) {
+        Frag<T> vB[NDT];
+        while (i < hi) {
+            get_k(kA, i + 2 * LANES);
+            get_v(vB, i + LANES);
+            use(kB, vA);
+            i += LANES;
+            if (i >= hi) break;
+            get_k(kB, i + 2 * LANES);
+            get_v(vA, i + LANES);
+            use(kA, vB);
+            i += LANES;
+        }
+    } else {
+        while (i < hi) {
+            get_v(vA, i);
+            use(kB, vA);
+            get_k(kB, i + 2 * LANES);
+            i += LANES;
+        }
+    }
+}
+
+// The key lanes of a workgroup of 4 waves (4 lanes, or twice 2 of different parts) joined by log-sum-exp in lane order:
+// out(row, columns d.., O to the maximum, maximum, sum) for four columns of each row.  smem: DH x 256 bytes.
+template <typename T, int DH, int LANES, typename F>
+__device__ __forceinline__ void join_few(const WaveAttention<T, DH, 1>& w, unsigned char* smem, int rows, int wave4, int lane, F out) {
+    constexpr int NDT = DH / 16;
+    __shared__ float s_max4[4][16], s_sum4[4][16];
+    const int c = lane & 15, g = lane >> 4, wave = wave4 % LANES;
+    f32x4_t* s_o = reinterpret_cast<f32x4_t*>(smem) + (wave4 - wave) * NDT * 64;   // [lane][dt][64]
+    float (*s_max)[16] = s_max4 + wave4 - wave, (*s_sum)[16] = s_sum4 + wave4 - wave;
+    const float sum = across_rows(w.rsum[0], OpSum());
+    if (g == 0) {
+        s_max[wave][c] = w.rmax[0];
+        s_sum[wave][c] = sum;
+    }
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) s_o[(wave * NDT + dt) * 64 + lane] = w.o[0][dt];
+    __syncthreads();
+    if (c >= rows) return;
+    float wt[LANES], top = -INFINITY, den = 0.f;
+#pragma unroll
+    for (int k = 0; k < LANES; ++k) top = fmaxf(top, s_max[k][c]);
+#pragma unroll
+    for (int k = 0; k < LANES; ++k) {
+        const float m = s_max[k][c];
+        wt[k] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        den = fmaf(wt[k], s_sum[k][c], den);
+    }
+#pragma unroll
+    for (int i = 0; i < NDT / LANES; ++i) {
+        const int dt = wave + LANES * i;
+        f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < LANES; ++k) {
+            const f32x4_t ov = s_o[(k * NDT + dt) * 64 + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(ov[e], wt[k], acc[e]);
+        }
+        out(c, 16 * dt + 4 * g, acc, top, den);
+    }
+}
+
+// ------------------------------------------------------------------ 64 rows, K and V through LDS (bf16)
+template <int DH>
+struct TileShape {
+    static constexpr int CPR = DH / 8;                        // 16-byte chunks per K row
+    static constexpr int HALF = 32 * DH * 2, BLK = 2 * HALF;  // bytes of a block's K (or V), of both
+    static constexpr int STAGE = kPrefixLanes * BLK;          // a step's blocks, one per key lane
+};
+
+// The attention of rows row0 .. row0 + rows - 1 (at most 64) over blocks lo .. hi - 1 by 4 waves: wave 2 rs + kp has rows
+// 32 rs .. of key lane kp.  K's rows are stored with their 16-byte chunks permuted by row (applied to the source address),
+// so that 16 rows' same chunk lies in 16 different banks.  smem: two stages.
+template <int DH>
+__device__ __forceinline__ void attend_tile(WaveAttention<uint16_t, DH, 2>& w, const AttnArgs& at, const HeadCache<uint16_t>& hc,
+                                            int lo, int hi, int row0, int rows, int h, int m0, const Sight& see,
+                                            unsigned char* smem, int wave, int lane) {
+    using T = uint16_t;
+    using S = TileShape<DH>;
+    constexpr int NDS = DH / 32, NDT = DH / 16, PIECES = S::HALF / 1024 / 2;   // 1 KiB loads per operand and wave
+    const int rs = wave >> 1, kp = wave & 1, c = lane & 15, g = lane >> 4;
+    const int nstep = (hi - lo + 1) / 2;
+    auto swz = [](int row) { return S::CPR == 16 ? row & 15 : (row >> 1) & 7; };
+    // waves 0, 1 load lane 0's block, waves 2, 3 lane 1's, half of its K and of its V each
+    uint32_t ko[PIECES], vo[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int piece = (wave & 1) * PIECES + i, ch = piece * 64 + lane, row = ch / S::CPR;
+        vo[i] = (uint32_t)piece * 1024;
+        ko[i] = (uint32_t)(row * S::CPR + ((ch % S::CPR) ^ swz(row))) * 16;
+    }
+    auto request = [&](int step) {   // a block past the last repeats it: in bounds, never used
+        const int j = min(lo + 2 * step + (wave >> 1), hi - 1);
+        const bool shared = j < hc.pages;
+        const unsigned char* kb = reinterpret_cast<const unsigned char*>(shared ? hc.k0 : hc.k1) + (size_t)j * S::HALF;
+        const unsigned char* vb = reinterpret_cast<const unsigned char*>(shared ? hc.v0 : hc.v1) + (size_t)j * S::HALF;
+        unsigned char* dst = smem + (step & 1) * S::STAGE + (wave >> 1) * S::BLK;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + ko[i]),
+                                             (__attribute__((address_space(3))) void*)(dst + vo[i]), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + vo[i] + lane * 16),
+                                             (__attribute__((address_space(3))) void*)(dst + S::HALF + vo[i]), 16, 0, 0);
+        }
+    };
+    w.clear();
+    if (nstep <= 0) return;
+    request(0);
+    Frag<T> qh[2][NDS], ql[2][NDS];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int r = min(32 * rs + 16 * t + c, rows - 1);   // rows past the last repeat it
+        const float* q0 = at.qbuf + ((size_t)(row0 + r) * at.H + h) * DH + 8 * g;
+#pragma unroll
+        for (int ds = 0; ds < NDS; ++ds) query_frag<T>(at, q0 + 32 * ds, qh[t][ds], ql[t][ds]);
+    }
+    const bool idle = 32 * rs >= rows;
+    for (int i = 0; i < nstep; ++i) {
+        // this wave's loads of step i have landed; after the barrier everyone's have, and nobody still reads the other stage
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(7 << 4);   // vmcnt 0, lgkmcnt 0
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (i + 1 < nstep) request(i + 1);
+        const int blk = lo + 2 * i + kp;
+        if (blk >= hi || idle) continue;
+        const unsigned char* sk = smem + (i & 1) * S::STAGE + kp * S::BLK;
+        const unsigned char* sv = sk + S::HALF;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) w.s[t][0] = w.s[t][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ds = 0; ds < NDS; ++ds)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const int row = 16 * kt + c;
+                const Frag<T> kf =
+                    Frag<T>::load(reinterpret_cast<const T*>(sk + (row * S::CPR + ((ds * 4 + g) ^ swz(row))) * 16));
+#pragma unroll
+                for (int t = 0; t < 2; ++t) mma2(w.s[t][kt], kf, qh[t][ds], ql[t][ds]);
+            }
+        w.look(blk, m0 + 32 * rs, see, lane);
+        Frag<T> ph[2], pl[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) w.weigh(t, ph[t], pl[t]);
+        const bool junk = 32 * blk + 32 > see.Tb;   // keys that no row sees: their V may be anything
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
-            mma(o[t][dt], vf[dt], ph);
-            if constexpr (two) mma(o[t][dt], vf[dt], pl);
+            Frag<T> vf = Frag<T>::load(reinterpret_cast<const T*>(sv + (16 * dt + c) * 64 + g * 16));
+            if (junk) drop_keys<T>(vf, 32 * blk, g, see.Tb);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) mma2(w.o[t][dt], vf, ph[t], pl[t]);
         }
     }
 }
 
-// Blocks lo + wave, lo + wave + 4, ... below hi of the cache behind kr, vr.  A block past the wave's last is asked for
-// past the end of the buffer: no memory is read.
-template <typename T, int NDS, int NDT, int RT>
-__device__ __forceinline__ void attend_range(__amdgpu_buffer_rsrc_t kr, __amdgpu_buffer_rsrc_t vr, int none, int lo, int hi,
-                                             const Frag<T>* qs, int lane, int wave, int nt, int m0, const Sight& see,
-                                             float (&rmax)[RT], float (&rsum)[RT], f32x4_t (&o)[RT][NDT]) {
-    const int c = lane & 15, g = lane >> 4;
-    constexpr bool ahead = sizeof(T) == 2 || NDS == 2;   // float heads of 128: one block's registers are all there are
-    Frag<T> kA[2][NDS], vA[NDT];
-    if constexpr (ahead) {
-        Frag<T> kB[2][NDS], vB[NDT];
-        int i = lo + wave;
-        load_kv<T, NDS, NDT>(kA, vA, kr, vr, i < hi ? i : none, c, g, 0);
-        while (i < hi) {
-            const int j = i + kShareWaves, l = j + kShareWaves;
-            load_kv<T, NDS, NDT>(kB, vB, kr, vr, j < hi ? j : none, c, g, 0);
-            attend<T, NDS, NDT, RT>(kA, vA, qs, lane, nt, m0, see, i, rmax, rsum, o);
-            if (j >= hi) break;
-            load_kv<T, NDS, NDT>(kA, vA, kr, vr, l < hi ? l : none, c, g, 0);
-            attend<T, NDS, NDT, RT>(kB, vB, qs, lane, nt, m0, see, j, rmax, rsum, o);
-            i = l;
+// The key lanes joined by log-sum-exp in lane order, as join_few; smem: the stages.
+template <int DH, typename F>
+__device__ __forceinline__ void join_tile(const WaveAttention<uint16_t, DH, 2>& w, unsigned char* smem, int rows, int wave, int lane,
+                                          F out) {
+    constexpr int NDT = DH / 16;
+    static_assert(4 * 2 * NDT * 1024 <= 2 * TileShape<DH>::STAGE, "the waves' results fit the stages");
+    __shared__ float s_max[4][2][16], s_sum[4][2][16];
+    f32x4_t* s_o = reinterpret_cast<f32x4_t*>(smem);   // [wave][t][dt][lane]
+    const int rs = wave >> 1, kp = wave & 1, c = lane & 15, g = lane >> 4;
+    __syncthreads();   // the stages are free
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const float sum = across_rows(w.rsum[t], OpSum());
+        if (g == 0) {
+            s_max[wave][t][c] = w.rmax[t];
+            s_sum[wave][t][c] = sum;
         }
-    } else {
-        for (int i = lo + wave; i < hi; i += kShareWaves) {
-            load_kv<T, NDS, NDT>(kA, vA, kr, vr, i, c, g, 0);
-            attend<T, NDS, NDT, RT>(kA, vA, qs, lane, nt, m0, see, i, rmax, rsum, o);
-        }
-    }
-}
-
-template <typename T, int DH, int RT, bool WHOLE>
-__global__ void __launch_bounds__(64 * kShareWaves, RT == 4 ? 1 : 2) shared_attn_kernel(SharedArgs a) {
-    constexpr int NDS = DH / 32, NDT = DH / 16, P = sizeof(T) == 2 ? 2 : 1, TILE = 16 * RT;
-    constexpr int Q_BYTES = RT * P * NDS * 64 * (int)sizeof(Frag<T>), M_BYTES = kShareWaves * NDT * 64 * 16;
-    __shared__ __align__(16) unsigned char smem[Q_BYTES > M_BYTES ? Q_BYTES : M_BYTES];
-    __shared__ float s_max[RT][kShareWaves][16], s_sum[RT][kShareWaves][16];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int c = lane & 15, g = lane >> 4;
-    const AttnArgs& at = a.at;
-    const int q = at.q, n = a.group;
-
-    // the workgroup's part: rows row0 .. row0 + rows - 1 of the batch (nt tiles), key blocks of two caches
-    int h, grp, b, row0, rows, m0, slot, lo, hi;
-    bool prefix;
-    if (!WHOLE && (int)blockIdx.x < a.prefix_grid) {
-        // the row tiles of a part are neighbours on one XCD (workgroups go to the 8 of them in turn)
-        const int x = blockIdx.x & 7, y = blockIdx.x >> 3, tile = y % a.tiles, part = (y / a.tiles) * 8 + x;
-        slot = part % a.prefix_parts;
-        h = part / a.prefix_parts % at.H;
-        grp = part / a.prefix_parts / at.H;
-        if (grp * n >= at.B) return;
-        lo = slot * a.chunk;
-        hi = min(lo + a.chunk, a.pages[grp]);
-        if (lo >= hi) return;   // a shorter prefix than the longest group's: the join skips the part too
-        b = grp * n;
-        m0 = tile * TILE;
-        row0 = b * q + m0;
-        rows = min(TILE, n * q - m0);
-        prefix = true;
-    } else {
-        int i = WHOLE ? (int)blockIdx.x : (int)blockIdx.x - a.prefix_grid;
-        const int part = WHOLE ? 0 : i % a.own_parts;
-        if (!WHOLE) i /= a.own_parts;
-        const int tiles = (q + TILE - 1) / TILE;
-        const int tile = i % tiles;
-        i /= tiles;
-        h = i % at.H;
-        b = i / at.H;
-        grp = b / n;
-        m0 = tile * TILE;
-        row0 = b * q + m0;
-        rows = min(TILE, q - m0);
-        slot = a.prefix_parts + part;
-        lo = a.pages[grp] + part * a.own_chunk;
-        hi = !WHOLE && part < a.own_parts - 1 ? lo + a.own_chunk : 0x7FFFFFF;   // the last part runs on to the true end
-        prefix = false;
-    }
-    const int nt = (rows + 15) / 16;
-
-    // the rows' queries, scaled into units of log 2, as fragments in LDS (rows past the last repeat it)
-    Frag<T>* s_q = reinterpret_cast<Frag<T>*>(smem);
-    for (int i = threadIdx.x; i < RT * NDS * 64; i += 64 * kShareWaves) {
-        const int t = i / (NDS * 64), ds = i / 64 % NDS, r = min(16 * t + (i & 15), rows - 1);
-        if (t >= nt) break;
-        const f32x4u_t* src = reinterpret_cast<const f32x4u_t*>(at.qbuf + ((size_t)(row0 + r) * at.H + h) * DH + 32 * ds +
-                                                                8 * ((i >> 4) & 3));
-        const f32x4u_t q0 = src[0], q1 = src[1];
-        const float x8[8] = {q0.x * at.scale, q0.y * at.scale, q0.z * at.scale, q0.w * at.scale,
-                             q1.x * at.scale, q1.y * at.scale, q1.z * at.scale, q1.w * at.scale};
-        Frag<T> hi8, lo8;
-        split_frag<T>(x8, hi8, lo8);
-        s_q[(t * P * NDS + ds) * 64 + (i & 63)] = hi8;
-        if constexpr (P == 2) s_q[(t * P * NDS + NDS + ds) * 64 + (i & 63)] = lo8;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) s_o[((wave * 2 + t) * NDT + dt) * 64 + lane] = w.o[t][dt];
     }
     __syncthreads();
-
-    float rmax[RT], rsum[RT];
-    f32x4_t o[RT][NDT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        rmax[t] = -INFINITY;
-        rsum[t] = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) o[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-    const uint32_t bytes = (uint32_t)at.S_max * DH * sizeof(T);
-    const int none = at.S_max / 32;
-    if (prefix || WHOLE) {
-        const size_t off = ((size_t)grp * n * at.H + h) * at.S_max * DH;
-        const Sight all{0x7FFFFFFF, 0x7FFFFFFF, 0, nullptr};
-        attend_range<T, NDS, NDT, RT>(buf_rsrc(reinterpret_cast<const T*>(at.kc) + off, bytes),
-                                      buf_rsrc(reinterpret_cast<const T*>(at.vc) + off, bytes), none, WHOLE ? 0 : lo,
-                                      WHOLE ? a.pages[grp] : hi, s_q, lane, wave, nt, m0, all, rmax, rsum, o);
-    }
-    if (!prefix) {
-        const int L = at.cache_len[b];
-        const bool over = L < 0 || L + q > at.S_max;   // the host checks capacity; never read past this sequence's cache
-        if (threadIdx.x == 0 && (over || L < 32 * a.pages[grp])) atomicOr(at.err, over ? 4 : 16);
-        const int nblk = over ? 0 : (L + min(m0 + TILE, q) + 31) / 32;   // what the tile's last row can see
-        const size_t off = ((size_t)b * at.H + h) * at.S_max * DH;
-        const Sight see{L, L + q, q, at.mask ? at.mask + (size_t)b * q : nullptr};
-        attend_range<T, NDS, NDT, RT>(buf_rsrc(reinterpret_cast<const T*>(at.kc) + off, bytes),
-                                      buf_rsrc(reinterpret_cast<const T*>(at.vc) + off, bytes), none, lo, min(hi, nblk),
-                                      s_q, lane, wave, nt, m0, see, rmax, rsum, o);
-    }
-
-    // the waves' results joined by log-sum-exp in wave order, tile by tile through LDS
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        rsum[t] += __shfl_xor(rsum[t], 16, 64);
-        rsum[t] += __shfl_xor(rsum[t], 32, 64);
-        if (g == 0) {
-            s_max[t][wave][c] = rmax[t];
-            s_sum[t][wave][c] = rsum[t];
-        }
-    }
-    f32x4_t* s_o = reinterpret_cast<f32x4_t*>(smem);   // [wave][dt][lane], in place of Q
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        if (t >= nt) break;
-        __syncthreads();
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) s_o[(wave * NDT + dt) * 64 + lane] = o[t][dt];
-        __syncthreads();
-        const int r = 16 * t + c;
-        float w[kShareWaves], top = -INFINITY, den = 0.f;
-#pragma unroll
-        for (int k = 0; k < kShareWaves; ++k) top = fmaxf(top, s_max[t][k][c]);
-#pragma unroll
-        for (int k = 0; k < kShareWaves; ++k) {
-            const float m = s_max[t][k][c];
-            w[k] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-            den = fmaf(w[k], s_sum[t][k][c], den);
-        }
+    for (int t = 0; t < 2; ++t) {
+        const int r = 32 * rs + 16 * t + c;
         if (r >= rows) continue;
+        float wt[2], top = -INFINITY, den = 0.f;
 #pragma unroll
-        for (int i = 0; i < NDT / kShareWaves; ++i) {
-            const int dt = wave + kShareWaves * i, d = 16 * dt + 4 * g;
+        for (int k = 0; k < 2; ++k) top = fmaxf(top, s_max[2 * rs + k][t][c]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float m = s_max[2 * rs + k][t][c];
+            wt[k] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+            den = fmaf(wt[k], s_sum[2 * rs + k][t][c], den);
+        }
+#pragma unroll
+        for (int i = 0; i < NDT / 2; ++i) {
+            const int dt = kp + 2 * i;
             f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < kShareWaves; ++k) {
-                const f32x4_t ov = s_o[(k * NDT + dt) * 64 + lane];
+            for (int k = 0; k < 2; ++k) {
+                const f32x4_t ov = s_o[(((2 * rs + k) * 2 + t) * NDT + dt) * 64 + lane];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = fmaf(ov[e], w[k], acc[e]);
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(ov[e], wt[k], acc[e]);
             }
-            if constexpr (WHOLE) {
-                const float inv = den == 0.f ? 0.f : 1.0f / den;   // a row that sees no key: zeros
-                store_out<T>(at, out_off<DH>(at, b, h, m0 + r, d), acc * inv);
-            } else {
-                float* pr = a.part + (((size_t)(row0 + r) * at.H + h) * a.slots + slot) * (DH + 4);
-                *reinterpret_cast<f32x4_t*>(pr + d) = acc;
-                if (dt == 0 && g == 0) *reinterpret_cast<float2*>(pr + DH) = float2{top, den};
-            }
+            out(r, 16 * dt + 4 * g, acc, top, den);
         }
     }
 }
 
-// Joins the parts of each row and head: DH / 4 threads each, four columns per thread.
+// ------------------------------------------------------------------ kernels
+// A prefix part: head, group, pages and rows of unit `unit` (part and row tile); false where it has none.  The row tiles
+// of a part are neighbours on one XCD (workgroups go to the 8 of them in turn).
+struct PrefixPart { int h, b, lo, hi, row0, rows, slot; };
+__device__ __forceinline__ bool prefix_part(const SharedArgs& a, int unit, int tile_rows, PrefixPart& p) {
+    const int x = unit & 7, y = unit >> 3, tile = y % a.tiles, part = (y / a.tiles) * 8 + x;
+    const int grp = part / a.prefix_parts / a.at.H;
+    p.slot = part % a.prefix_parts;
+    p.h = part / a.prefix_parts % a.at.H;
+    p.b = grp * a.group;
+    if (p.b >= a.at.B) return false;
+    p.lo = p.slot * a.chunk;
+    p.hi = min(p.lo + a.chunk, a.pages[grp]);
+    p.row0 = p.b * a.at.q + tile * tile_rows;
+    p.rows = min(tile_rows, a.group * a.at.q - tile * tile_rows);
+    return p.lo < p.hi;   // else a shorter prefix than the longest group's: the join skips the part too
+}
+
+template <int DH>
+__device__ __forceinline__ void store_part(const SharedArgs& a, int row, int h, int slot, int d, f32x4_t acc, float top, float den) {
+    float* pr = a.part + (((size_t)row * a.at.H + h) * a.slots + slot) * (DH + 4);
+    *reinterpret_cast<f32x4_t*>(pr + d) = acc;
+    if (d == 0) *reinterpret_cast<float2*>(pr + DH) = float2{top, den};
+}
+
+// The rows of a block of sequence b that a workgroup has, of head h.
+struct OwnRows { int h, b, m0, row0, rows, pages; };
+__device__ __forceinline__ OwnRows own_rows(const SharedArgs& a, int i, int tile, int tile_rows) {
+    OwnRows o;
+    o.h = i % a.at.H;
+    o.b = i / a.at.H;
+    o.m0 = tile * tile_rows;
+    o.row0 = o.b * a.at.q + o.m0;
+    o.rows = min(tile_rows, a.at.q - o.m0);
+    o.pages = a.pages[o.b / a.group];
+    return o;
+}
+// Key blocks of sequence b (rows up to m of its block): none where the cache is too short (the host checks capacity;
+// never read past this sequence's cache).
+__device__ __forceinline__ int key_blocks(const SharedArgs& a, int L, int m) {
+    return L < 0 || L + a.at.q > a.at.S_max ? 0 : (L + min(m, a.at.q) + 31) / 32;
+}
+__device__ __forceinline__ void report(const SharedArgs& a, int L, int pages) {
+    const bool over = L < 0 || L + a.at.q > a.at.S_max;
+    if (threadIdx.x == 0 && (over || L < 32 * pages)) atomicOr(a.at.err, over ? 4 : 16);
+}
+__device__ __forceinline__ Sight own_sight(const SharedArgs& a, int b, int L) {
+    return {L, L + a.at.q, a.at.q, a.at.mask ? a.at.mask + (size_t)b * a.at.q : nullptr};
+}
+
+// The parts: workgroups of the prefix, then those of the own slots.
+template <typename T, int DH, bool STAGED>
+__global__ void __launch_bounds__(256, 2) shared_parts_kernel(SharedArgs a) {
+    __shared__ __align__(1024) unsigned char smem[STAGED ? 2 * TileShape<DH>::STAGE : DH * 256];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if ((int)blockIdx.x < a.prefix_grid) {
+        PrefixPart p;
+        auto store = [&](int r, int d, f32x4_t acc, float top, float den) {
+            store_part<DH>(a, p.row0 + r, p.h, p.slot, d, acc, top, den);
+        };
+        const Sight all{0x7FFFFFFF, 0x7FFFFFFF, 0, nullptr};
+        if constexpr (STAGED) {
+            if (!prefix_part(a, blockIdx.x, kTileRows, p)) return;
+            WaveAttention<T, DH, 2> w;
+            attend_tile<DH>(w, a.at, head_cache<T, DH>(a.at, p.b, p.b, p.h, 0), p.lo, p.hi, p.row0, p.rows, p.h, 0, all, smem,
+                            wave, lane);
+            join_tile<DH>(w, smem, p.rows, wave, lane, store);
+        } else {
+            // two units: waves 0, 1 and waves 2, 3 (of neighbours on one XCD)
+            const int unit = ((int)blockIdx.x >> 3) * 16 + (wave >> 1) * 8 + (blockIdx.x & 7);
+            const bool any = prefix_part(a, unit, 16, p);
+            WaveAttention<T, DH, 1> w;
+            w.clear();
+            if (any)
+                attend_few<T, DH, kPrefixLanes>(w, a.at, head_cache<T, DH>(a.at, p.b, p.b, p.h, 0), p.lo, p.hi, p.row0, p.rows,
+                                                p.h, 0, wave & 1, lane, [&](int&) { return all; });
+            join_few<T, DH, kPrefixLanes>(w, smem, any ? p.rows : 0, wave, lane, store);
+        }
+        return;
+    }
+    const int tiles = (a.at.q + 15) / 16, i = (int)blockIdx.x - a.prefix_grid, part = i % a.own_parts, j = i / a.own_parts;
+    const OwnRows o = own_rows(a, j / tiles, j % tiles, 16);
+    const int lo = o.pages + part * a.own_chunk;
+    WaveAttention<T, DH, 1> w;
+    attend_few<T, DH, kOwnLanes>(w, a.at, head_cache<T, DH>(a.at, o.b, o.b, o.h, 0), lo, min(lo + a.own_chunk, a.at.S_max / 32),
+                                 o.row0, o.rows, o.h, o.m0, wave, lane, [&](int& hi) {
+        const int L = a.at.cache_len[o.b];
+        if (part == 0) report(a, L, o.pages);
+        hi = min(hi, key_blocks(a, L, a.at.q));
+        return own_sight(a, o.b, L);
+    });
+    join_few<T, DH, kOwnLanes>(w, smem, o.rows, wave, lane, [&](int r, int d, f32x4_t acc, float top, float den) {
+        store_part<DH>(a, o.row0 + r, o.h, a.prefix_parts + part, d, acc, top, den);
+    });
+}
+
+// Joins the parts of each row and head, DH / 4 threads with four columns each: parts that hold no key of the row (maximum
+// -inf) count nothing.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) shared_join_kernel(SharedArgs a) {
-    constexpr int D4 = DH / 4;
-    const AttnArgs& at = a.at;
-    const int e = (int)(blockIdx.x * 256 + threadIdx.x);
-    const int rh = e / D4, d = 4 * (e % D4), row = rh / at.H, h = rh % at.H;
-    if (row >= at.B * at.q) return;
-    const int b = row / at.q, pages = a.pages[b / a.group];
-    const int np = (pages + a.chunk - 1) / a.chunk;   // the group's prefix parts
+    constexpr int D4 = DH / 4, U = 8;   // parts whose loads are in flight together
+    const int e = (int)(blockIdx.x * 256 + threadIdx.x), rh = e / D4, d = 4 * (e % D4), row = rh / a.at.H, h = rh % a.at.H;
+    if (row >= a.at.B * a.at.q) return;
+    const int b = row / a.at.q, np = (a.pages[b / a.group] + a.chunk - 1) / a.chunk, all = np + a.own_parts;
     const float* base = a.part + (size_t)rh * a.slots * (DH + 4);
-    float top = -INFINITY;
-    for (int i = 0; i < a.slots; ++i)
-        if (i < np || i >= a.prefix_parts) top = fmaxf(top, base[(size_t)i * (DH + 4) + DH]);
-    float den = 0.f;
-    f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < a.slots; ++i) {
-        if (i >= np && i < a.prefix_parts) continue;
-        const float* pr = base + (size_t)i * (DH + 4);
-        const float2 ms = *reinterpret_cast<const float2*>(pr + DH);
-        const f32x4_t ov = *reinterpret_cast<const f32x4_t*>(pr + d);
-        const float w = ms.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms.x - top);
-        den = fmaf(w, ms.y, den);
+    f32x4_t sum = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float total = 0.f, top = -INFINITY;
+    for (int k = 0; k < all; k += U) {   // past the last it is read again
+        f32x4_t ov[U];
+        float2 ms[U];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) acc[k] = fmaf(ov[k], w, acc[k]);
+        for (int u = 0; u < U; ++u) {
+            const int i = min(k + u, all - 1);
+            const float* pr = base + (size_t)(i < np ? i : a.prefix_parts + i - np) * (DH + 4);
+            ov[u] = *reinterpret_cast<const f32x4_t*>(pr + d);
+            ms[u] = *reinterpret_cast<const float2*>(pr + DH);
+        }
+        float m = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u) m = fmaxf(m, ms[u].x);
+        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - m);
+        top = m;
+        total *= f;
+        sum *= f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float wt = k + u >= all || ms[u].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[u].x - m);
+            total = fmaf(wt, ms[u].y, total);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = fmaf(ov[u][i], wt, sum[i]);
+        }
     }
-    const float inv = den == 0.f ? 0.f : 1.0f / den;   // a row that sees no key: zeros
-    store_out<T>(at, out_off<DH>(at, b, h, row - b * at.q, d), acc * inv);
+    const float inv = total == 0.f ? 0.f : 1.0f / total;   // a row that sees no key: zeros
+    store_out<T>(a.at, out_off<DH>(a.at, b, h, row - b * a.at.q, d), sum * inv);
+}
+
+// Blocks of more than kAttnSplitRows rows: prefix and own pages in one workgroup per row tile, the longest first.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256, 2) shared_rows_kernel(SharedArgs a) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    constexpr int TILE = sizeof(T) == 2 ? kTileRows : 16;
+    __shared__ __align__(1024) unsigned char smem[sizeof(T) == 2 ? 2 * TileShape<DH>::STAGE : DH * 256];
+    const OwnRows o = own_rows(a, (int)blockIdx.x / a.tiles, a.tiles - 1 - (int)blockIdx.x % a.tiles, TILE);
+    const int L = a.at.cache_len[o.b], nblk = key_blocks(a, L, o.m0 + TILE);   // what the tile's last row can see
+    report(a, L, o.pages);
+    const Sight see = own_sight(a, o.b, L);
+    const HeadCache<T> hc = head_cache<T, DH>(a.at, o.b / a.group * a.group, o.b, o.h, o.pages);
+    auto write = [&](int r, int d, f32x4_t acc, float, float den) {
+        const float inv = den == 0.f ? 0.f : 1.0f / den;   // a row that sees no key: zeros
+        store_out<T>(a.at, out_off<DH>(a.at, o.b, o.h, o.m0 + r, d), acc * inv);
+    };
+    if constexpr (sizeof(T) == 2) {
+        WaveAttention<T, DH, 2> w;
+        attend_tile<DH>(w, a.at, hc, 0, nblk, o.row0, o.rows, o.h, o.m0, see, smem, wave, lane);
+        join_tile<DH>(w, smem, o.rows, wave, lane, write);
+    } else {
+        WaveAttention<T, DH, 1> w;
+        attend_few<T, DH, 4>(w, a.at, hc, 0, nblk, o.row0, o.rows, o.h, o.m0, wave, lane, [&](int&) { return see; });
+        join_few<T, DH, 4>(w, smem, o.rows, wave, lane, write);
+    }
 }
 
 template <typename T, int DH>
 static hipError_t launch_shared_dh(const SharedPlan& p, const SharedArgs& a, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1) {
-    void (*kern)(SharedArgs);
+    auto go = [&](void (*kern)(SharedArgs), size_t grid, hipEvent_t begin, hipEvent_t end) {
+        if (begin || end) hipExtLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, begin, end, 0, a);
+        else hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, a);
+        return hipGetLastError();
+    };
+    if (p.whole) return go(shared_rows_kernel<T, DH>, p.grid, ev0, ev1);
+    void (*parts)(SharedArgs) = shared_parts_kernel<T, DH, false>;
     if constexpr (sizeof(T) == 2) {
-        if (p.whole) kern = shared_attn_kernel<T, DH, 4, true>;   // more than 64 rows: four tiles
-        else if (p.rt == 4) kern = shared_attn_kernel<T, DH, 4, false>;
-        else if (p.rt == 2) kern = shared_attn_kernel<T, DH, 2, false>;
-        else kern = shared_attn_kernel<T, DH, 1, false>;
-    } else {
-        kern = p.whole ? shared_attn_kernel<T, DH, 1, true> : shared_attn_kernel<T, DH, 1, false>;
+        if (p.staged) parts = shared_parts_kernel<T, DH, true>;
     }
-    const dim3 block(64 * kShareWaves);
-    if (ev0) hipExtLaunchKernelGGL(kern, dim3(p.grid), block, 0, s, ev0, p.whole ? ev1 : nullptr, 0, a);
-    else hipLaunchKernelGGL(kern, dim3(p.grid), block, 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.whole) return e;
-    const unsigned grid = (unsigned)(((size_t)a.at.B * a.at.q * a.at.H * (DH / 4) + 255) / 256);
-    if (ev1) hipExtLaunchKernelGGL((shared_join_kernel<T, DH>), dim3(grid), dim3(256), 0, s, nullptr, ev1, 0, a);
-    else hipLaunchKernelGGL((shared_join_kernel<T, DH>), dim3(grid), dim3(256), 0, s, a);
-    return hipGetLastError();
+    const hipError_t e = go(parts, p.grid, ev0, nullptr);
+    if (e != hipSuccess) return e;
+    return go(shared_join_kernel<T, DH>, ((size_t)a.at.B * a.at.q * a.at.H * (DH / 4) + 255) / 256, nullptr, ev1);
 }
 
 hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p, SharedArgs a, hipStream_t s, hipEvent_t ev0,
@@ -430,14 +684,13 @@ hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p,
     if (at.q < 1 || at.q > 4096 || (at.mask && at.q > 64) || at.B < 1 || at.H < 1 || a.group < 1 || at.B % a.group ||
         at.B / a.group > kMaxShareGroups || at.S_max < 32 || at.S_max % 32 || at.ldo % 4 || !at.qbuf || !at.kc || !at.vc ||
         !at.cache_len || !at.out || !at.err || p.whole != (at.q > kAttnSplitRows) || (!p.whole && !a.part) ||
-        (dtype == 1 ? p.rt != 4 && (p.whole || (p.rt != 1 && p.rt != 2)) : p.rt != 1))
+        (dtype != 1 && p.staged) || (dtype == 1 && p.whole && !p.staged))
         return hipErrorInvalidValue;
     for (int g = 0; g < at.B / a.group; ++g)
         if (a.pages[g] < 0 || a.pages[g] > at.S_max / 32 || (!p.whole && a.pages[g] > p.chunk * p.prefix_parts))
             return hipErrorInvalidValue;
     a.chunk = p.chunk; a.prefix_parts = p.prefix_parts; a.own_chunk = p.own_chunk; a.own_parts = p.own_parts;
     a.slots = p.slots; a.tiles = p.tiles; a.prefix_grid = p.prefix_grid;
-    if (p.whole) a.chunk = a.prefix_parts = a.own_parts = 1;
     if (dtype == 1) {
         if (head_dim == 128) return launch_shared_dh<uint16_t, 128>(p, a, s, ev0, ev1);
         if (head_dim == 64) return launch_shared_dh<uint16_t, 64>(p, a, s, ev0, ev1);

@@ -144,6 +144,7 @@ hipError_t launch_attention_rows(int dtype, int head_dim, const AttnArgs& a, hip
 // and counter unused.  The launch fills the rest from its plan.
 constexpr int kMaxShareGroups = 64;
 constexpr int kSharedParts = 512;      // workgroups the shared pages (one row tile) and the own pages are cut into, about
+constexpr int kSharedFewRows = 32;     // groups of more rows stage K and V in LDS (bf16)
 constexpr int kSharedMaxParts = 32;    // parts of a prefix, at most
 constexpr int kSharedMaxOwn = 8;       // parts of a sequence's own slots, at most
 struct SharedArgs {
@@ -155,7 +156,9 @@ struct SharedArgs {
 };
 struct SharedPlan {
     bool whole;                        // blocks of more than kAttnSplitRows rows: no parts
-    int rt, chunk, prefix_parts, own_chunk, own_parts, slots, tiles, own_tiles, prefix_grid, grid;
+    bool staged;                       // workgroups of 64 rows, else of 16
+    // pages of a prefix part, parts; pages of an own part, parts; parts of a row; row tiles; workgroups of the prefix, of all
+    int chunk, prefix_parts, own_chunk, own_parts, slots, tiles, prefix_grid, grid;
 };
 SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pages, int max_len, int S_max);
 size_t shared_partial_floats(const SharedPlan& p, int B, int q, int H, int head_dim);

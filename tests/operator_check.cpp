@@ -38,25 +38,25 @@ int main() {
                             for (int len : {32 * most, 32 * most + 45, c.S - q}) {
                                 if (len < 32 * most || len + q > c.S) continue;
                                 const SharedPlan p = plan_shared(B, group, c.H, q, dtype, pages.data(), len, c.S);
-                                const int rows = 16 * p.rt;
-                                CHECK(p.rt == 1 || (dtype == 1 && (p.rt == 4 || (!p.whole && p.rt == 2))), "no instance: rt %d",
-                                      p.rt);
-                                CHECK(p.whole == (q > kAttnSplitRows), "whole at q %d", q);
+                                const int rows = p.staged ? 64 : 16;
+                                CHECK(p.whole == (q > kAttnSplitRows) && (dtype == 1 || !p.staged) && (p.staged || dtype == 0 || !p.whole),
+                                      "kind of workgroup at q %d", q);
                                 if (p.whole) {
-                                    CHECK(p.grid == B * c.H * ((q + rows - 1) / rows), "grid of a long block, q %d", q);
+                                    CHECK(p.grid == B * c.H * p.tiles && p.tiles == (q + rows - 1) / rows, "grid of a long block, q %d", q);
                                     continue;
                                 }
                                 CHECK(shared_partial_floats(p, B, q, c.H, c.Dh) <= have, "parts: B %d group %d q %d need %zu have %zu",
                                       B, group, q, shared_partial_floats(p, B, q, c.H, c.Dh), have);
                                 // every page of every group, and every own page up to the length, has a part
+                                const int least = *std::min_element(pages.begin(), pages.end());
                                 CHECK(p.chunk * p.prefix_parts >= most && p.own_chunk >= 1 && p.own_parts >= 1 &&
+                                          p.own_parts * p.own_chunk >= (len + q + 31) / 32 - least &&
                                           p.slots == p.prefix_parts + p.own_parts,
                                       "parts: %d x %d for %d pages", p.chunk, p.prefix_parts, most);
-                                CHECK(p.tiles * rows >= group * q && p.own_tiles * rows >= q, "row tiles: q %d group %d", q, group);
-                                CHECK(p.prefix_grid % 8 == 0 &&
-                                          p.prefix_grid >= (int)pages.size() * c.H * p.prefix_parts * p.tiles &&
-                                          p.grid == p.prefix_grid + B * c.H * p.own_tiles * p.own_parts,
-                                      "grid: %d of %d", p.prefix_grid, p.grid);
+                                CHECK(p.tiles * rows >= group * q && p.prefix_grid % 8 == 0 &&
+                                          p.prefix_grid * (p.staged ? 1 : 2) >= (int)pages.size() * c.H * p.prefix_parts * p.tiles &&
+                                          p.grid == p.prefix_grid + B * c.H * ((q + 15) / 16) * p.own_parts,
+                                      "grid: %d, %d tiles", p.grid, p.tiles);
                                 // the key ranges do not follow the block's rows or the committed length
                                 CHECK(p.chunk == one.chunk && p.own_chunk == one.own_chunk && p.prefix_parts == one.prefix_parts,
                                       "key ranges vary with the block: B %d q %d len %d", B, q, len);
@@ -92,10 +92,10 @@ int main() {
         a = args(6); a.at.ldo = 130; bad("an odd row stride", 1, 64, a, p);
         a = args(6); a.at.qbuf = nullptr; bad("no queries", 1, 64, a, p);
         a = args(65); bad("a decode plan for a long block", 1, 64, a, p);
-        SharedPlan r = p; r.rt = 2; bad("two row tiles of floats", 0, 64, args(6), r);
+        SharedPlan r = p; r.staged = true; bad("staged floats", 0, 64, args(6), r);
         const SharedPlan w = plan_shared(4, 2, 2, 65, 1, pages, 140, 256);
         a = args(65); a.at.mask = reinterpret_cast<const uint64_t*>(ptr); bad("masks of a long block", 1, 64, a, w);
-        r = w; r.rt = 1; bad("one row tile of a long bf16 block", 1, 64, args(65), r);
+        r = w; r.staged = false; bad("a long bf16 block that is not staged", 1, 64, args(65), r);
     }
     // reordering
     {
