@@ -197,13 +197,6 @@ struct WaveAttention {
     }
 };
 
-// acc += a * (hi + lo)
-template <typename T>
-__device__ __forceinline__ void mma2(f32x4_t& acc, const Frag<T>& a, const Frag<T>& hi, const Frag<T>& lo) {
-    mma(acc, a, hi);
-    if constexpr (sizeof(T) == 2) mma(acc, a, lo);
-}
-
 // The cache rows of a head that an attention reads: pages below `pages` from the group's first sequence, the others from
 // the sequence itself.
 template <typename T>
@@ -274,8 +267,13 @@ __device__ __forceinline__ void attend_few(WaveAttention<T, DH, 1>& w, const Att
         w.s[0][0] = w.s[0][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ds = 0; ds < NDS; ++ds) {
-            mma2(w.s[0][0], kf[0][ds], qh[ds], ql[ds]);
-            mma2(w.s[0][1], kf[1][ds], qh[ds], ql[ds]);
+            // products that follow each other go to different sums: each waits for its sum's last one
+            mma(w.s[0][0], kf[0][ds], qh[ds]);
+            mma(w.s[0][1], kf[1][ds], qh[ds]);
+            if constexpr (E == 2) {
+                mma(w.s[0][0], kf[0][ds], ql[ds]);
+                mma(w.s[0][1], kf[1][ds], ql[ds]);
+            }
         }
     };
     // block i, its scores formed: K of the next block in kn, V in v
@@ -289,7 +287,11 @@ __device__ __forceinline__ void attend_few(WaveAttention<T, DH, 1>& w, const Att
         w.weigh(0, ph, pl);
         score(kn);
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) mma2(w.o[0][dt], v[dt], ph, pl);
+        for (int dt = 0; dt < NDT; ++dt) mma(w.o[0][dt], v[dt], ph);
+        if constexpr (E == 2) {
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) mma(w.o[0][dt], v[dt], pl);
+        }
     };
     score(kA);
     if constexpr (ahead) {
@@ -316,14 +318,14 @@ __device__ __forceinline__ void attend_few(WaveAttention<T, DH, 1>& w, const Att
 }
 
 // The key lanes of a workgroup of 4 waves (4 lanes, or twice 2 of different parts) joined by log-sum-exp in lane order:
-// out(row, columns d.., O to the maximum, maximum, sum) for four columns of each row.  smem: DH x 256 bytes.
+// out(row, columns d.., O to the maximum, maximum, sum) for four columns of each row.  smem: FewBytes.
+template <int DH> constexpr int FewBytes = DH * 256 + 2 * 4 * 16 * 4;
 template <typename T, int DH, int LANES, typename F>
 __device__ __forceinline__ void join_few(const WaveAttention<T, DH, 1>& w, unsigned char* smem, int rows, int wave4, int lane, F out) {
     constexpr int NDT = DH / 16;
-    __shared__ float s_max4[4][16], s_sum4[4][16];
     const int c = lane & 15, g = lane >> 4, wave = wave4 % LANES;
     f32x4_t* s_o = reinterpret_cast<f32x4_t*>(smem) + (wave4 - wave) * NDT * 64;   // [lane][dt][64]
-    float (*s_max)[16] = s_max4 + wave4 - wave, (*s_sum)[16] = s_sum4 + wave4 - wave;
+    float (*s_max)[16] = reinterpret_cast<float (*)[16]>(smem + DH * 256) + wave4 - wave, (*s_sum)[16] = s_max + 4;
     const float sum = across_rows(w.rsum[0], OpSum());
     if (g == 0) {
         s_max[wave][c] = w.rmax[0];
@@ -357,12 +359,98 @@ __device__ __forceinline__ void join_few(const WaveAttention<T, DH, 1>& w, unsig
 }
 
 // ------------------------------------------------------------------ 64 rows, K and V through LDS (bf16)
+// The kernels that load into LDS hold one shared array: with several, the compiler takes every read of LDS for one that may
+// depend on the loads in flight and waits for them.
 template <int DH>
 struct TileShape {
     static constexpr int CPR = DH / 8;                        // 16-byte chunks per K row
     static constexpr int HALF = 32 * DH * 2, BLK = 2 * HALF;  // bytes of a block's K (or V), of both
     static constexpr int STAGE = kPrefixLanes * BLK;          // a step's blocks, one per key lane
+    static constexpr int BYTES = 2 * STAGE + 1024;            // two stages, and the rows' maxima and sums
+    __device__ __forceinline__ static int swz(int row) { return CPR == 16 ? row & 15 : (row >> 1) & 7; }
 };
+
+// One block for a wave's 32 rows, from a stage's K and V, while the next step's blocks come into the other stage (pieces
+// at offsets ko of its K and vo of its V).
+template <int DH>
+__device__ __forceinline__ void tile_step(WaveAttention<uint16_t, DH, 2>& w, unsigned char* next, const unsigned char* stage, bool load, bool use,
+                                          const unsigned char* kb, const unsigned char* vb,
+                                          const uint32_t (&ko)[DH / 32], const uint32_t (&vo)[DH / 32],
+                                          const Frag<uint16_t> (&qh)[2][DH / 32], const Frag<uint16_t> (&ql)[2][DH / 32], int blk,
+                                          int m0, const Sight& see, int lane) {
+    using T = uint16_t;
+    using S = TileShape<DH>;
+    constexpr int NDS = DH / 32, NDT = DH / 16, PIECES = DH / 32;
+    const int c = lane & 15, g = lane >> 4;
+    if (load) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + ko[i]),
+                                             (__attribute__((address_space(3))) void*)(next + vo[i]), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + vo[i] + lane * 16),
+                                             (__attribute__((address_space(3))) void*)(next + S::HALF + vo[i]), 16, 0, 0);
+        }
+    }
+    if (!use) return;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) w.s[t][0] = w.s[t][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // K and V fragments are read one product group ahead of their use (the scheduler would move the reads next to it)
+    auto k_frags = [&](Frag<T> (&kf)[2], int ds) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const int row = 16 * kt + c;
+            kf[kt] = Frag<T>::load(reinterpret_cast<const T*>(stage + (row * S::CPR + ((ds * 4 + g) ^ S::swz(row))) * 16));
+        }
+    };
+    const bool junk = 32 * blk + 32 > see.Tb;   // keys that no row sees: their V may be anything
+    auto v_frags = [&](Frag<T> (&vf)[2], int dt) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            vf[u] = Frag<T>::load(reinterpret_cast<const T*>(stage + S::HALF + (16 * (dt + u) + c) * 64 + g * 16));
+    };
+    Frag<T> f[2][2];
+    k_frags(f[0], 0);
+#pragma unroll
+    for (int ds = 0; ds < NDS; ++ds) {
+        const Frag<T> (&kf)[2] = f[ds & 1];
+        if (ds + 1 < NDS) k_frags(f[(ds + 1) & 1], ds + 1);
+        else v_frags(f[(ds + 1) & 1], 0);
+        __builtin_amdgcn_sched_barrier(0);
+        // products that follow each other go to different sums: each waits for its sum's last one
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) mma(w.s[t][kt], kf[kt], qh[t][ds]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) mma(w.s[t][kt], kf[kt], ql[t][ds]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    w.look(blk, m0, see, lane);
+    Frag<T> ph[2], pl[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) w.weigh(t, ph[t], pl[t]);
+#pragma unroll
+    for (int dt = 0; dt < NDT; dt += 2) {
+        Frag<T> (&vf)[2] = f[(NDS + dt / 2) & 1];
+        if (dt + 2 < NDT) v_frags(f[(NDS + dt / 2 + 1) & 1], dt + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        if (junk) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) drop_keys<T>(vf[u], 32 * blk, g, see.Tb);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) mma(w.o[t][dt + u], vf[u], ph[t]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) mma(w.o[t][dt + u], vf[u], pl[t]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 
 // The attention of rows row0 .. row0 + rows - 1 (at most 64) over blocks lo .. hi - 1 by 4 waves: wave 2 rs + kp has rows
 // 32 rs .. of key lane kp.  K's rows are stored with their 16-byte chunks permuted by row (applied to the source address),
@@ -373,36 +461,30 @@ __device__ __forceinline__ void attend_tile(WaveAttention<uint16_t, DH, 2>& w, c
                                             unsigned char* smem, int wave, int lane) {
     using T = uint16_t;
     using S = TileShape<DH>;
-    constexpr int NDS = DH / 32, NDT = DH / 16, PIECES = S::HALF / 1024 / 2;   // 1 KiB loads per operand and wave
+    constexpr int NDS = DH / 32, PIECES = DH / 32;   // 1 KiB loads per operand and wave
     const int rs = wave >> 1, kp = wave & 1, c = lane & 15, g = lane >> 4;
     const int nstep = (hi - lo + 1) / 2;
-    auto swz = [](int row) { return S::CPR == 16 ? row & 15 : (row >> 1) & 7; };
     // waves 0, 1 load lane 0's block, waves 2, 3 lane 1's, half of its K and of its V each
     uint32_t ko[PIECES], vo[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
         const int piece = (wave & 1) * PIECES + i, ch = piece * 64 + lane, row = ch / S::CPR;
         vo[i] = (uint32_t)piece * 1024;
-        ko[i] = (uint32_t)(row * S::CPR + ((ch % S::CPR) ^ swz(row))) * 16;
+        ko[i] = (uint32_t)(row * S::CPR + ((ch % S::CPR) ^ S::swz(row))) * 16;
     }
-    auto request = [&](int step) {   // a block past the last repeats it: in bounds, never used
-        const int j = min(lo + 2 * step + (wave >> 1), hi - 1);
+    Frag<T> qh[2][NDS], ql[2][NDS];
+    // step i: its block is used (i >= 0), step i + 1's requested; a block past the last repeats it: in bounds, never used
+    auto step = [&](int i) {
+        const int j = min(lo + 2 * (i + 1) + (wave >> 1), hi - 1), blk = lo + 2 * i + kp;
         const bool shared = j < hc.pages;
         const unsigned char* kb = reinterpret_cast<const unsigned char*>(shared ? hc.k0 : hc.k1) + (size_t)j * S::HALF;
         const unsigned char* vb = reinterpret_cast<const unsigned char*>(shared ? hc.v0 : hc.v1) + (size_t)j * S::HALF;
-        unsigned char* dst = smem + (step & 1) * S::STAGE + (wave >> 1) * S::BLK;
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + ko[i]),
-                                             (__attribute__((address_space(3))) void*)(dst + vo[i]), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + vo[i] + lane * 16),
-                                             (__attribute__((address_space(3))) void*)(dst + S::HALF + vo[i]), 16, 0, 0);
-        }
+        tile_step<DH>(w, smem + ((i + 1) & 1) * S::STAGE + (wave >> 1) * S::BLK, smem + (i & 1) * S::STAGE + kp * S::BLK,
+                      i + 1 < nstep, i >= 0 && blk < hi && 32 * rs < rows, kb, vb, ko, vo, qh, ql, blk, m0 + 32 * rs, see, lane);
     };
     w.clear();
     if (nstep <= 0) return;
-    request(0);
-    Frag<T> qh[2][NDS], ql[2][NDS];
+    step(-1);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int r = min(32 * rs + 16 * t + c, rows - 1);   // rows past the last repeat it
@@ -410,7 +492,6 @@ __device__ __forceinline__ void attend_tile(WaveAttention<uint16_t, DH, 2>& w, c
 #pragma unroll
         for (int ds = 0; ds < NDS; ++ds) query_frag<T>(at, q0 + 32 * ds, qh[t][ds], ql[t][ds]);
     }
-    const bool idle = 32 * rs >= rows;
     for (int i = 0; i < nstep; ++i) {
         // this wave's loads of step i have landed; after the barrier everyone's have, and nobody still reads the other stage
         asm volatile("" ::: "memory");
@@ -418,35 +499,7 @@ __device__ __forceinline__ void attend_tile(WaveAttention<uint16_t, DH, 2>& w, c
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (i + 1 < nstep) request(i + 1);
-        const int blk = lo + 2 * i + kp;
-        if (blk >= hi || idle) continue;
-        const unsigned char* sk = smem + (i & 1) * S::STAGE + kp * S::BLK;
-        const unsigned char* sv = sk + S::HALF;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) w.s[t][0] = w.s[t][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ds = 0; ds < NDS; ++ds)
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                const int row = 16 * kt + c;
-                const Frag<T> kf =
-                    Frag<T>::load(reinterpret_cast<const T*>(sk + (row * S::CPR + ((ds * 4 + g) ^ swz(row))) * 16));
-#pragma unroll
-                for (int t = 0; t < 2; ++t) mma2(w.s[t][kt], kf, qh[t][ds], ql[t][ds]);
-            }
-        w.look(blk, m0 + 32 * rs, see, lane);
-        Frag<T> ph[2], pl[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) w.weigh(t, ph[t], pl[t]);
-        const bool junk = 32 * blk + 32 > see.Tb;   // keys that no row sees: their V may be anything
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) {
-            Frag<T> vf = Frag<T>::load(reinterpret_cast<const T*>(sv + (16 * dt + c) * 64 + g * 16));
-            if (junk) drop_keys<T>(vf, 32 * blk, g, see.Tb);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) mma2(w.o[t][dt], vf, ph[t], pl[t]);
-        }
+        step(i);
     }
 }
 
@@ -456,8 +509,8 @@ __device__ __forceinline__ void join_tile(const WaveAttention<uint16_t, DH, 2>& 
                                           F out) {
     constexpr int NDT = DH / 16;
     static_assert(4 * 2 * NDT * 1024 <= 2 * TileShape<DH>::STAGE, "the waves' results fit the stages");
-    __shared__ float s_max[4][2][16], s_sum[4][2][16];
     f32x4_t* s_o = reinterpret_cast<f32x4_t*>(smem);   // [wave][t][dt][lane]
+    float (*s_max)[2][16] = reinterpret_cast<float (*)[2][16]>(smem + 2 * TileShape<DH>::STAGE), (*s_sum)[2][16] = s_max + 4;
     const int rs = wave >> 1, kp = wave & 1, c = lane & 15, g = lane >> 4;
     __syncthreads();   // the stages are free
 #pragma unroll
@@ -552,7 +605,7 @@ __device__ __forceinline__ Sight own_sight(const SharedArgs& a, int b, int L) {
 // The parts: workgroups of the prefix, then those of the own slots.
 template <typename T, int DH, bool STAGED>
 __global__ void __launch_bounds__(256, 2) shared_parts_kernel(SharedArgs a) {
-    __shared__ __align__(1024) unsigned char smem[STAGED ? 2 * TileShape<DH>::STAGE : DH * 256];
+    __shared__ __align__(1024) unsigned char smem[STAGED ? TileShape<DH>::BYTES : FewBytes<DH>];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if ((int)blockIdx.x < a.prefix_grid) {
         PrefixPart p;
@@ -585,7 +638,7 @@ __global__ void __launch_bounds__(256, 2) shared_parts_kernel(SharedArgs a) {
     WaveAttention<T, DH, 1> w;
     attend_few<T, DH, kOwnLanes>(w, a.at, head_cache<T, DH>(a.at, o.b, o.b, o.h, 0), lo, min(lo + a.own_chunk, a.at.S_max / 32),
                                  o.row0, o.rows, o.h, o.m0, wave, lane, [&](int& hi) {
-        const int L = a.at.cache_len[o.b];
+        const int L = __builtin_amdgcn_readfirstlane(a.at.cache_len[o.b]);
         if (part == 0) report(a, L, o.pages);
         hi = min(hi, key_blocks(a, L, a.at.q));
         return own_sight(a, o.b, L);
@@ -640,9 +693,9 @@ template <typename T, int DH>
 __global__ void __launch_bounds__(256, 2) shared_rows_kernel(SharedArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     constexpr int TILE = sizeof(T) == 2 ? kTileRows : 16;
-    __shared__ __align__(1024) unsigned char smem[sizeof(T) == 2 ? 2 * TileShape<DH>::STAGE : DH * 256];
+    __shared__ __align__(1024) unsigned char smem[sizeof(T) == 2 ? TileShape<DH>::BYTES : FewBytes<DH>];
     const OwnRows o = own_rows(a, (int)blockIdx.x / a.tiles, a.tiles - 1 - (int)blockIdx.x % a.tiles, TILE);
-    const int L = a.at.cache_len[o.b], nblk = key_blocks(a, L, o.m0 + TILE);   // what the tile's last row can see
+    const int L = __builtin_amdgcn_readfirstlane(a.at.cache_len[o.b]), nblk = key_blocks(a, L, o.m0 + TILE);   // what the tile's last row can see
     report(a, L, o.pages);
     const Sight see = own_sight(a, o.b, L);
     const HeadCache<T> hc = head_cache<T, DH>(a.at, o.b / a.group * a.group, o.b, o.h, o.pages);
