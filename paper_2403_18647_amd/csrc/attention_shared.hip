@@ -25,8 +25,7 @@
 // (rows in lanes, keys in registers and lane groups), and O^T += V^T P^T takes P
 // as it stands.  Two kinds of workgroup do this, with the same values:
 //  * few rows, and float models: a wave per key lane and 16 rows, K and V
-//    straight from the cache into registers, the next block's in flight and its
-//    scores formed beside the present one's softmax; bound by HBM;
+//    straight from the cache into registers; bound by HBM;
 //  * many rows of bf16 models: 64 rows, two key lanes of two waves with 32 rows
 //    each; the blocks go straight into LDS while the ones before are used, Q
 //    stays in registers; bound by the matrix cores.
@@ -214,8 +213,7 @@ __device__ __forceinline__ HeadCache<T> head_cache(const AttnArgs& at, int first
 
 // Eight query columns scaled into units of log 2, as value and remainder.
 template <typename T>
-__device__ __forceinline__ void query_frag(const AttnArgs& at, const float* q8, Frag<T>& hi, Frag<T>& lo) {
-    const f32x4u_t a = reinterpret_cast<const f32x4u_t*>(q8)[0], b = reinterpret_cast<const f32x4u_t*>(q8)[1];
+__device__ __forceinline__ void query_frag(const AttnArgs& at, f32x4u_t a, f32x4u_t b, Frag<T>& hi, Frag<T>& lo) {
     const float x[8] = {a.x * at.scale, a.y * at.scale, a.z * at.scale, a.w * at.scale,
                         b.x * at.scale, b.y * at.scale, b.z * at.scale, b.w * at.scale};
     split_frag<T>(x, hi, lo);
@@ -223,19 +221,33 @@ __device__ __forceinline__ void query_frag(const AttnArgs& at, const float* q8, 
 
 // ------------------------------------------------------------------ 16 rows, K and V from the cache to registers
 // The attention of rows row0 .. row0 + rows - 1 (at most 16) over blocks from lo, a wave per key lane (`wave` of LANES).
-// The first blocks are requested (below hi) before the queries and before late(hi) says what the rows see and where the
-// blocks end; a block past the wave's last is asked for past the end of the buffer, which reads no memory.
+// K of the next block is requested as soon as the scores of the present one are formed, V of the next after its products:
+// one block's registers, so that three waves share a SIMD and one's loads fill the others' waits.  Loads return in order:
+// the sequence's length (len, null for a prefix) and the queries are asked for ahead of the first block, which is
+// requested below hi before late(length, hi) says what the rows see and where the blocks end; a block past the wave's
+// last is asked for past the end of the buffer, which reads no memory.
 template <typename T, int DH, int LANES, typename F>
 __device__ __forceinline__ void attend_few(WaveAttention<T, DH, 1>& w, const AttnArgs& at, const HeadCache<T>& hc, int lo, int hi,
-                                           int row0, int rows, int h, int m0, int wave, int lane, F late) {
+                                           int row0, int rows, int h, int m0, int wave, int lane, const int* len, F late) {
     constexpr int NDS = DH / 32, NDT = DH / 16;
     constexpr uint32_t E = sizeof(T);
-    constexpr bool ahead = E == 2 || DH == 64;   // float heads of 128: the registers hold one block's V
     const int c = lane & 15, g = lane >> 4, none = at.S_max / 32;
     const uint32_t bytes = (uint32_t)at.S_max * DH * E;
     const __amdgpu_buffer_rsrc_t k0 = buf_rsrc(hc.k0, bytes), v0 = buf_rsrc(hc.v0, bytes), k1 = buf_rsrc(hc.k1, bytes),
                                  v1 = buf_rsrc(hc.v1, bytes);
-    auto get_k = [&](Frag<T> (&kf)[2][NDS], int j) {
+    int zero = 0;
+    asm volatile("" : "+v"(zero));   // a vector load: a scalar one would be placed behind the requests
+    const int L = len ? len[zero] : 0;
+    f32x4u_t q8[NDS][2];
+    {
+        const float* q0 = at.qbuf + ((size_t)(row0 + min(c, rows - 1)) * at.H + h) * DH + 8 * g;   // rows past the last repeat it
+#pragma unroll
+        for (int ds = 0; ds < NDS; ++ds)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) q8[ds][u] = reinterpret_cast<const f32x4u_t*>(q0 + 32 * ds)[u];
+    }
+    Frag<T> kf[2][NDS], vf[NDT], qh[NDS], ql[NDS];
+    auto get_k = [&](int j) {
         const __amdgpu_buffer_rsrc_t r = j < hc.pages ? k0 : k1;
         const int blk = j < hi ? j : none;
 #pragma unroll
@@ -245,25 +257,21 @@ __device__ __forceinline__ void attend_few(WaveAttention<T, DH, 1>& w, const Att
             for (int ds = 0; ds < NDS; ++ds) kf[kt][ds] = buf_frag<T>(r, ko, ds * 32 * E);
         }
     };
-    auto get_v = [&](Frag<T> (&vf)[NDT], int j) {
+    auto get_v = [&](int j) {
         const __amdgpu_buffer_rsrc_t r = j < hc.pages ? v0 : v1;
         const uint32_t vo = ((uint32_t)(j < hi ? j : none) * DH * 32 + c * 32 + 8 * g) * E;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) vf[dt] = buf_frag<T>(r, vo, dt * 16 * 32 * E);
     };
-    Frag<T> kA[2][NDS], kB[2][NDS], vA[NDT], qh[NDS], ql[NDS];
     int i = lo + wave;
-    get_k(kA, i);
-    if constexpr (ahead) get_v(vA, i);
-    get_k(kB, i + LANES);
-    {
-        const float* q0 = at.qbuf + ((size_t)(row0 + min(c, rows - 1)) * at.H + h) * DH + 8 * g;   // rows past the last repeat it
+    get_k(i);
+    get_v(i);
+    __builtin_amdgcn_sched_barrier(0);   // the requests stay ahead of the wait for the queries
 #pragma unroll
-        for (int ds = 0; ds < NDS; ++ds) query_frag<T>(at, q0 + 32 * ds, qh[ds], ql[ds]);
-    }
+    for (int ds = 0; ds < NDS; ++ds) query_frag<T>(at, q8[ds][0], q8[ds][1], qh[ds], ql[ds]);
     w.clear();
-    const Sight see = late(hi);
-    auto score = [&](const Frag<T> (&kf)[2][NDS]) {
+    const Sight see = late(__builtin_amdgcn_readfirstlane(L), hi);
+    for (; i < hi; i += LANES) {
         w.s[0][0] = w.s[0][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ds = 0; ds < NDS; ++ds) {
@@ -275,45 +283,23 @@ __device__ __forceinline__ void attend_few(WaveAttention<T, DH, 1>& w, const Att
                 mma(w.s[0][1], kf[1][ds], ql[ds]);
             }
         }
-    };
-    // block i, its scores formed: K of the next block in kn, V in v
-    auto use = [&](const Frag<T> (&kn)[2][NDS], Frag<T> (&v)[NDT]) {
+        __builtin_amdgcn_sched_barrier(0);
+        get_k(i + LANES);
         w.look(i, m0, see, lane);
         if (32 * i + 32 > see.Tb) {   // keys that no row sees: their V may be anything
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) drop_keys<T>(v[dt], 32 * i, g, see.Tb);
+            for (int dt = 0; dt < NDT; ++dt) drop_keys<T>(vf[dt], 32 * i, g, see.Tb);
         }
         Frag<T> ph, pl;
         w.weigh(0, ph, pl);
-        score(kn);
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) mma(w.o[0][dt], v[dt], ph);
+        for (int dt = 0; dt < NDT; ++dt) mma(w.o[0][dt], vf[dt], ph);
         if constexpr (E == 2) {
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) mma(w.o[0][dt], v[dt], pl);
+            for (int dt = 0; dt < NDT; ++dt) mma(w.o[0][dt], vf[dt], pl);
         }
-    };
-    score(kA);
-    if constexpr (ahead) {
-        Frag<T> vB[NDT];
-        while (i < hi) {
-            get_k(kA, i + 2 * LANES);
-            get_v(vB, i + LANES);
-            use(kB, vA);
-            i += LANES;
-            if (i >= hi) break;
-            get_k(kB, i + 2 * LANES);
-            get_v(vA, i + LANES);
-            use(kA, vB);
-            i += LANES;
-        }
-    } else {
-        while (i < hi) {
-            get_v(vA, i);
-            use(kB, vA);
-            get_k(kB, i + 2 * LANES);
-            i += LANES;
-        }
+        __builtin_amdgcn_sched_barrier(0);
+        get_v(i + LANES);
     }
 }
 
@@ -484,14 +470,22 @@ __device__ __forceinline__ void attend_tile(WaveAttention<uint16_t, DH, 2>& w, c
     };
     w.clear();
     if (nstep <= 0) return;
-    step(-1);
+    f32x4u_t q8[2][NDS][2];   // loads return in order: the queries ahead of the first blocks
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int r = min(32 * rs + 16 * t + c, rows - 1);   // rows past the last repeat it
         const float* q0 = at.qbuf + ((size_t)(row0 + r) * at.H + h) * DH + 8 * g;
 #pragma unroll
-        for (int ds = 0; ds < NDS; ++ds) query_frag<T>(at, q0 + 32 * ds, qh[t][ds], ql[t][ds]);
+        for (int ds = 0; ds < NDS; ++ds)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) q8[t][ds][u] = reinterpret_cast<const f32x4u_t*>(q0 + 32 * ds)[u];
     }
+    step(-1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int ds = 0; ds < NDS; ++ds) query_frag<T>(at, q8[t][ds][0], q8[t][ds][1], qh[t][ds], ql[t][ds]);
     for (int i = 0; i < nstep; ++i) {
         // this wave's loads of step i have landed; after the barrier everyone's have, and nobody still reads the other stage
         asm volatile("" ::: "memory");
@@ -604,7 +598,7 @@ __device__ __forceinline__ Sight own_sight(const SharedArgs& a, int b, int L) {
 
 // The parts: workgroups of the prefix, then those of the own slots.
 template <typename T, int DH, bool STAGED>
-__global__ void __launch_bounds__(256, 2) shared_parts_kernel(SharedArgs a) {
+__global__ void __launch_bounds__(256, STAGED || sizeof(T) * DH > 256 ? 2 : 3) shared_parts_kernel(SharedArgs a) {
     __shared__ __align__(1024) unsigned char smem[STAGED ? TileShape<DH>::BYTES : FewBytes<DH>];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if ((int)blockIdx.x < a.prefix_grid) {
@@ -627,7 +621,7 @@ __global__ void __launch_bounds__(256, 2) shared_parts_kernel(SharedArgs a) {
             w.clear();
             if (any)
                 attend_few<T, DH, kPrefixLanes>(w, a.at, head_cache<T, DH>(a.at, p.b, p.b, p.h, 0), p.lo, p.hi, p.row0, p.rows,
-                                                p.h, 0, wave & 1, lane, [&](int&) { return all; });
+                                                p.h, 0, wave & 1, lane, nullptr, [&](int, int&) { return all; });
             join_few<T, DH, kPrefixLanes>(w, smem, any ? p.rows : 0, wave, lane, store);
         }
         return;
@@ -637,8 +631,7 @@ __global__ void __launch_bounds__(256, 2) shared_parts_kernel(SharedArgs a) {
     const int lo = o.pages + part * a.own_chunk;
     WaveAttention<T, DH, 1> w;
     attend_few<T, DH, kOwnLanes>(w, a.at, head_cache<T, DH>(a.at, o.b, o.b, o.h, 0), lo, min(lo + a.own_chunk, a.at.S_max / 32),
-                                 o.row0, o.rows, o.h, o.m0, wave, lane, [&](int& hi) {
-        const int L = __builtin_amdgcn_readfirstlane(a.at.cache_len[o.b]);
+                                 o.row0, o.rows, o.h, o.m0, wave, lane, a.at.cache_len + o.b, [&](int L, int& hi) {
         if (part == 0) report(a, L, o.pages);
         hi = min(hi, key_blocks(a, L, a.at.q));
         return own_sight(a, o.b, L);
@@ -709,7 +702,7 @@ __global__ void __launch_bounds__(256, 2) shared_rows_kernel(SharedArgs a) {
         join_tile<DH>(w, smem, o.rows, wave, lane, write);
     } else {
         WaveAttention<T, DH, 1> w;
-        attend_few<T, DH, 4>(w, a.at, hc, 0, nblk, o.row0, o.rows, o.h, o.m0, wave, lane, [&](int&) { return see; });
+        attend_few<T, DH, 4>(w, a.at, hc, 0, nblk, o.row0, o.rows, o.h, o.m0, wave, lane, nullptr, [&](int, int&) { return see; });
         join_few<T, DH, 4>(w, smem, o.rows, wave, lane, write);
     }
 }
