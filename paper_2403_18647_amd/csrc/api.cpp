@@ -123,7 +123,7 @@ struct sdsat_ctx {
     float* gemm_part = nullptr;   // partial rows of split residual GEMMs
     float* shared_part = nullptr; // parts of shared-prefix attention
     size_t shared_part_floats = 0;
-    int* reorder_steps = nullptr; // the copy list of a cache reordering
+    int* reorder_steps = nullptr; // cache reordering: arrival counts (zero between launches), copy list
     void* lp_part = nullptr;      // log probabilities: results of the segments of a row, and (zero between launches) how
     int* lp_ctr = nullptr;        // many have arrived
     int* cache_len = nullptr; int* err_flag = nullptr; int* verify_cnt = nullptr;
@@ -219,7 +219,7 @@ void carve(sdsat_ctx* c, Carver& cv) {
     }
     c->shared_part_floats = shared_partial_floats_most(D.maxB, D.H, D.maxQ, D.Dh);
     c->shared_part = (float*)cv.take(c->shared_part_floats * 4);
-    c->reorder_steps = (int*)cv.take((2 + 6 * (size_t)D.maxB) * 4);
+    c->reorder_steps = (int*)cv.take((kReorderHead + 6 * (size_t)D.maxB) * 4);
     c->lp_part = cv.take(logprob_part_bytes(D.maxM, D.V));
     c->lp_ctr = (int*)cv.take((size_t)D.maxM * 4);
     c->cache_len = (int*)cv.take((size_t)D.maxB * 4);
@@ -706,6 +706,7 @@ int sdsat_init(const sdsat_config* cfg, const void* const* weights, int32_t n_we
         (void)launch_fill_i32(c->verify_cnt, (size_t)((int*)(c->verify_best + D.maxM) - c->verify_cnt), 0, c->stream);
         (void)launch_fill_i32(c->attn_ctr, attention_counter_ints(D.maxB, D.H, D.maxQ), 0, c->stream);
         (void)launch_fill_i32(c->lp_ctr, (size_t)D.maxM, 0, c->stream);
+        (void)launch_fill_i32(c->reorder_steps, kReorderHead, 0, c->stream);
         (void)launch_fill_i32(c->cache_len, D.maxB, 0, c->stream);
         (void)launch_fill_i32(c->err_flag, 1, 0, c->stream);
         if (hipStreamSynchronize(c->stream) != hipSuccess) {

@@ -67,9 +67,9 @@ SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pag
         p.grid = B * H * p.tiles;
         return p;
     }
-    // pages per prefix part: two for each lane at the least, and parts enough for kSharedParts workgroups
+    // pages per prefix part: four for each lane at the least, and parts enough for kSharedParts workgroups
     const int parts = std::min(kSharedMaxParts, std::max(1, kSharedParts / (G * H)));
-    p.chunk = std::max(2 * kPrefixLanes, (most + parts - 1) / parts);
+    p.chunk = std::max(4 * kPrefixLanes, (most + parts - 1) / parts);
     p.prefix_parts = (most + p.chunk - 1) / p.chunk;
     // pages per own part: the own slots of a full cache in as many parts as fit kSharedParts workgroups, 1024 slots at the
     // least

@@ -168,8 +168,9 @@ hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p,
 
 // ---------------------------------------------------------------- cache reordering
 // sequence b < batch continues from sequence src[b] (any of the `all`, -1: none): whole pages from first_slot's on,
-// up to max_len at the most, and the lengths.  steps: 2 + 6 * all ints
-constexpr int kReorderMaxBatch = 1024;
+// up to max_len at the most, and the lengths.  steps: kReorderHead ints, zero between launches (arrival counts, a cache
+// line each), and 6 * all
+constexpr int kReorderMaxBatch = 1024, kReorderCounts = 16, kReorderHead = 32 * (1 + kReorderCounts) + 32;
 hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n_layers, int batch, int all, int H, int Dh,
                           int S_max, int* cache_len, int max_len, const int* src, int first_slot, int* steps, int* err,
                           hipStream_t s);
