@@ -373,7 +373,7 @@ __device__ __forceinline__ void tile_step(WaveAttention<uint16_t, DH, 2>& w, uns
         for (int i = 0; i < PIECES; ++i) {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + ko[i]),
                                              (__attribute__((address_space(3))) void*)(next + vo[i]), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + vo[i] + lane * 16),
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + vo[i] + c * 64 + g * 16),
                                              (__attribute__((address_space(3))) void*)(next + S::HALF + vo[i]), 16, 0, 0);
         }
     }
@@ -392,7 +392,7 @@ __device__ __forceinline__ void tile_step(WaveAttention<uint16_t, DH, 2>& w, uns
     auto v_frags = [&](Frag<T> (&vf)[2], int dt) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-            vf[u] = Frag<T>::load(reinterpret_cast<const T*>(stage + S::HALF + (16 * (dt + u) + c) * 64 + g * 16));
+            vf[u] = Frag<T>::load(reinterpret_cast<const T*>(stage + S::HALF + (dt + u) * 1024 + lane * 16));
     };
     Frag<T> f[2][2];
     k_frags(f[0], 0);
@@ -440,7 +440,7 @@ __device__ __forceinline__ void tile_step(WaveAttention<uint16_t, DH, 2>& w, uns
 
 // The attention of rows row0 .. row0 + rows - 1 (at most 64) over blocks lo .. hi - 1 by 4 waves: wave 2 rs + kp has rows
 // 32 rs .. of key lane kp.  K's rows are stored with their 16-byte chunks permuted by row (applied to the source address),
-// so that 16 rows' same chunk lies in 16 different banks.  smem: two stages.
+// so that 16 rows' same chunk lies in 16 different banks; V's fragments lie as the lanes read them.  smem: two stages.
 template <int DH>
 __device__ __forceinline__ void attend_tile(WaveAttention<uint16_t, DH, 2>& w, const AttnArgs& at, const HeadCache<uint16_t>& hc,
                                             int lo, int hi, int row0, int rows, int h, int m0, const Sight& see,
