@@ -50,6 +50,13 @@ static constexpr float kRaise = 8.f;
 static constexpr int kPrefixLanes = 2, kOwnLanes = 4;   // key lanes
 static constexpr int kTileRows = 64;                    // rows of a workgroup that stages K and V in LDS
 
+// Parts of all groups and heads.  More of them bring more waves where rows are few, fewer of them fewer partial results
+// where there are many: of one group over 6000 shared slots, 32 heads of 128, us per call with 256, 384 and 512 parts:
+// 2 sequences of 6 rows 32.4, 26.8, 31.3; 4 of 1 row 33.7, 30.8, 31.6; 12 of 6 rows 47.6, 54.1, 55.4; over 4000 slots, 16
+// of 6 rows 42.9, 50.0, 52.0; 32 of 6 rows 73.2, 78.3, 86.4.  The rows of a block have no say (16 of 1 row: 46.4, 39.0,
+// 39.9), so large groups are cut for speculative blocks.
+static int shared_parts(int group) { return group < kSharedMany ? kSharedParts : kSharedManyParts; }
+
 SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pages, int max_len, int S_max) {
     SharedPlan p{};
     const int G = B / group;
@@ -67,14 +74,13 @@ SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pag
         p.grid = B * H * p.tiles;
         return p;
     }
-    // pages per prefix part: four for each lane at the least, and parts enough for kSharedParts workgroups
-    const int parts = std::min(kSharedMaxParts, std::max(1, kSharedParts / (G * H)));
+    // pages per prefix part: four for each lane at the least
+    const int parts = std::min(kSharedMaxParts, std::max(1, shared_parts(group) / (G * H)));
     p.chunk = std::max(4 * kPrefixLanes, (most + parts - 1) / parts);
     p.prefix_parts = (most + p.chunk - 1) / p.chunk;
-    // pages per own part: the own slots of a full cache in as many parts as fit kSharedParts workgroups, 1024 slots at the
-    // least
+    // pages per own part: the own slots of a full cache in as many parts as that allows, 1024 slots at the least
     const int cap = S_max / 32 - least;
-    const int own = std::min(kSharedMaxOwn, std::max(1, kSharedParts / (B * H)));
+    const int own = std::min(kSharedMaxOwn, std::max(1, shared_parts(group) / (B * H)));
     p.own_chunk = std::max(32, (cap + own - 1) / own);
     const int nblk = std::max(1, std::min(cap, (max_len + q + 31) / 32 - least));
     p.own_parts = (nblk + p.own_chunk - 1) / p.own_chunk;

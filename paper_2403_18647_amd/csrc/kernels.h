@@ -143,7 +143,9 @@ hipError_t launch_attention_rows(int dtype, int head_dim, const AttnArgs& a, hip
 // group's first sequence; `at` as above with scale in units of log 2 (times log2 e), its splits, per_split, cols, part
 // and counter unused.  The launch fills the rest from its plan.
 constexpr int kMaxShareGroups = 64;
-constexpr int kSharedParts = 512;      // workgroups the shared pages (one row tile) and the own pages are cut into, about
+constexpr int kSharedParts = 384;      // parts the shared pages of all groups and heads are cut into, about; and the own pages
+constexpr int kSharedManyParts = 256;  // the same for groups of kSharedMany sequences or more
+constexpr int kSharedMany = 16;
 constexpr int kSharedFewRows = 32;     // groups of more rows stage K and V in LDS (bf16)
 constexpr int kSharedMaxParts = 32;    // parts of a prefix, at most
 constexpr int kSharedMaxOwn = 8;       // parts of a sequence's own slots, at most
