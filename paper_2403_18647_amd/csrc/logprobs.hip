@@ -13,16 +13,24 @@
 // A row is one segment, or several where there are few rows; one workgroup
 // streams each.  Its threads keep their own running maximum, sum and weighted
 // sum (no exchange while data arrives) and join them at the end.  For the n_top
-// largest, the lanes' running maxima serve: at least n_top of the wave's ids
-// reach the n_top-th largest of its 64 lanes' maxima, so only ids that do (and
-// exceed what earlier ids had set, ties going to the lower id) are candidates,
-// a few times n_top for logits in no order.  They are gathered in LDS as 64-bit
-// keys (the logit as an order-preserving integer above the complement of the
-// id: all differ, and ties need no care), thinned by the n_top-th largest of 64
-// groups of threads, and each is ranked by counting the larger ones.  Segments
-// with more candidates than LDS holds (many equal values, rising values) take
-// their ids one after the other.  The segment that arrives last joins the row's
-// results in segment order.
+// largest, the threads' maxima serve: at least n_top ids reach the n_top-th
+// largest maximum of 64 groups of 4 threads, so only ids that do are candidates,
+// little more than n_top for logits in no order, and only threads whose own
+// maximum does have any.  The workgroup reads those threads' ids once more (from
+// a cache), gathers the candidates in LDS as 64-bit keys (the logit as an
+// order-preserving integer above the complement of the id: all differ, and ties
+// need no care), and ranks each by counting the larger ones.  Segments with more
+// candidates than LDS holds (many equal values) take their ids one after the
+// other.  The segment that arrives last joins the row's results in segment order.
+//
+// Bound by HBM over many rows: 2047 rows of 32016 ids with one alternative take
+// 50 us, 5.2 TB/s (a large copy here reaches 4.9, a read 6.3).  Over few rows the
+// way from the last load to the result counts: 96 rows of 128256 ids take 17.7 us
+// with 20 alternatives and 12.3 with none, 8 to 10 of which the logits need; 6
+// rows of 32016 with 5 take 8.3, an empty launch 4.4.  There a workgroup runs each
+// part of its code for the first time, and what is short counts more than what is
+// unrolled: picking candidates while the logits stream, with its code in each of
+// the loop's tiles, took 22.3 us for the 96 rows and 57 for the 2047.
 #include <algorithm>
 
 #include "device.h"
@@ -34,11 +42,11 @@ static constexpr int kLpNT = 256, kLpWaves = kLpNT / 64;
 static constexpr int kLpVec = 4;                              // vector loads per thread and tile
 static constexpr int kLpTile = 64 * 4 * kLpVec;               // ids a wave takes at a time
 static constexpr int kLpStep = kLpWaves * kLpTile;            // segments are multiples of it
-static constexpr int kLpCand = 384;                           // candidates of a wave, at most
 static constexpr int kLpFew = 384;                            // candidates of a segment that are ranked, at most
-static constexpr int kLpGrid = 1024;                          // rows are cut into as many segments together, at most
+static constexpr int kLpGrid = 1024;                          // rows are cut into as many segments together, at most: four
+                                                              // workgroups a CU; 96 rows of 128256 took 24 us, with 2048 26
 static constexpr int kLpSegments = 64, kLpKeys = 1024;        // segments of a row, and their keys in the join, at most
-static_assert(kMaxTop <= 64 && kLpKeys <= kLpWaves * kLpCand, "lanes for the thresholds, LDS for the join");
+static_assert(kMaxTop <= 64, "lanes for the thresholds");
 
 typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));   // logits rows are float-aligned
 typedef unsigned long long u64;
@@ -95,7 +103,7 @@ __device__ __forceinline__ float nth_largest(float v, int n) {
     const uint32_t key = logit_key(v);
     u64 in = ~0ull;   // lanes whose leading bits are those of the n-th largest
     uint32_t got = 0;
-#pragma unroll
+#pragma unroll 4
     for (int b = 31; b >= 16; --b) {
         const u64 set = in & __ballot((key >> b) & 1u);
         const int k = __popcll(set);
@@ -140,40 +148,36 @@ struct LogprobArgs {
     const float* logits; int M, V, segs, seg;   // segments of a row, ids of each (the last takes the rest)
     const int* tokens; float inv_t; int n_top;
     float* lp; float* ent; int* ids; float* top_lp;
+    int tiles_log;                              // a segment is at most 2^tiles_log steps
     u64* part; u64* keys;                       // [M][segs][2]: the sums; [M][segs][n_top]: the largest keys
     int* counter;
     int per, per_inv;                           // join: first keys of each segment behind the threshold; ceil(2^16 / per)
     int* err;
 };
 
+// SMALL: fewer ids than a tile
+template <bool SMALL>
 __global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a) {
-    __shared__ u64 s_cand[kLpWaves * kLpCand];
+    __shared__ u64 s_cand[kLpKeys];
     __shared__ u64 s_top[kMaxTop], s_key[kLpWaves];   // the largest keys, in order
     __shared__ u64 s_few[kLpFew];
     __shared__ float s_group[64];
     __shared__ LpSums s_sums[kLpWaves];
-    __shared__ int s_count[kLpWaves], s_left, s_last;
+    __shared__ uint8_t s_from[kLpNT];
+    __shared__ int s_threads, s_left, s_last;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int row = (int)blockIdx.x / a.segs, sg = (int)blockIdx.x % a.segs, lo = sg * a.seg;
     const int n = min(a.seg, a.V - lo), n_top = a.n_top;
     const float* x = a.logits + (size_t)row * a.V + lo;
-    // the row's token and its logit, asked for now: only the row's last workgroup needs them
-    const int tok = a.lp ? a.tokens[row] : -1;
-    const float tok_x = tok >= 0 && tok < a.V ? a.logits[(size_t)row * a.V + tok] : 0.f;
-    if (tid == 0) s_left = 0;
-    if (lane == 0) s_count[wave] = 0;   // used by this wave alone while it streams
+    if (tid == 0) s_left = s_threads = 0;
     const float scale = a.inv_t * 1.44269504f;
 
-    // ids base + 256 i + 4 lane + j of the wave's tile at `base`; past the segment: -inf
+    // The wave's tile at `base`: ids first(base) + 256 i + 4 lane + j.  A tile that ends past the segment begins earlier, and
+    // `trim` takes out what belongs to the one before; of a tile behind the last, lane 0's part is read and not used: each
+    // tile is four loads, so that a wait for one leaves the next in flight
+    auto first = [&](int base) { return SMALL ? base : min(base, n - kLpTile); };
     auto load = [&](float (&v)[kLpVec][4], int base) {
-        if (base + kLpTile <= n) {
-#pragma unroll
-            for (int i = 0; i < kLpVec; ++i) {
-                const f32x4u_t t = *reinterpret_cast<const f32x4u_t*>(x + base + 256 * i + 4 * lane);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[i][j] = t[j];
-            }
-        } else {
+        if constexpr (SMALL) {
 #pragma unroll
             for (int i = 0; i < kLpVec; ++i)
 #pragma unroll
@@ -181,7 +185,23 @@ __global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a)
                     const int id = base + 256 * i + 4 * lane + j;
                     v[i][j] = id < n ? x[id] : -INFINITY;
                 }
+        } else {
+            const float* at = x + first(base) + (base < n ? 4 * lane : 0);
+#pragma unroll
+            for (int i = 0; i < kLpVec; ++i) {
+                const f32x4u_t t = *reinterpret_cast<const f32x4u_t*>(at + 256 * i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] = t[j];
+            }
         }
+    };
+    auto trim = [&](float (&v)[kLpVec][4], int base) {
+        if (SMALL || base + kLpTile <= n) return;
+#pragma unroll
+        for (int i = 0; i < kLpVec; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (base >= n || first(base) + 256 * i + 4 * lane + j < base) v[i][j] = -INFINITY;
     };
     LpSums r{-INFINITY, 0.f, 0.f};
     float ones = 0.f;                       // terms of 1 at the present maximum (none while it is -inf)
@@ -212,67 +232,26 @@ __global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a)
         ones += rintf(all - some);
         r.s += some;
         r.w += w;
-        return tm;
     };
-    // the tile's ids that reach `least` become candidates
-    const bool one_step = n <= kLpStep;
-    u64* cand = one_step ? s_few : s_cand + wave * kLpCand;
-    int* counter = one_step ? &s_left : &s_count[wave];
-    const int room = one_step ? kLpFew : kLpCand;
-    auto push = [&](const float (&v)[kLpVec][4], int base, float tm, float least) {
-        if (tm < least) return;
-        int c = 0;
-#pragma unroll
-        for (int i = 0; i < kLpVec; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) c += v[i][j] >= least;
-        int p = atomicAdd(counter, c);
-#pragma unroll
-        for (int i = 0; i < kLpVec; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (v[i][j] >= least) {
-                    if (p < room) cand[p] = id_key(v[i][j], lo + base + 256 * i + 4 * lane + j);
-                    ++p;
-                }
-    };
-    const float lowest = -3.402823466e38f;   // banned ids (-inf) are not taken
+    int tok = -1;
+    float tok_x;
     {
         float v0[kLpVec][4], v1[kLpVec][4];
         int base = wave * kLpTile;
         load(v0, base);
-        if (base + kLpStep < n) load(v1, base + kLpStep);
-        const float tm = add(v0);
-        float reach = -INFINITY;   // n_top ids of earlier tiles reach it
-        if (n_top > 0) {
-            // the first tiles of all waves: 64 groups of 4 threads
-            const float gm = across_quads(r.m, OpMax());
-            if ((lane & 3) == 0) s_group[tid >> 2] = gm;
-            __syncthreads();
-            reach = nth_largest(s_group[lane], n_top);
-            push(v0, base, tm, fmaxf(reach, lowest));
-        }
-        // later ids that only tie with what earlier ones reach lose
-        int k = 1;
-        auto later = [&](const float (&v)[kLpVec][4], int b) {
-            const float t = add(v);
-            if (n_top == 0) return;
-            float least = fmaxf(key_logit(logit_key(reach) + 1), lowest);
-            if ((k & 7) == 7 && (k & (k + 1)) == 0) {   // tiles 7, 15, 31, ..: the wave alone has seen more than the first tiles held
-                const float now = nth_largest(r.m, n_top);
-                if (now > reach) least = reach = now;
-            }
-            push(v, b, t, least);
-            ++k;
-        };
-        base += kLpStep;
+        // the row's token and its logit, asked for now: only the row's last workgroup needs them
+        if (a.lp) tok = a.tokens[row];
+        tok_x = a.logits[(size_t)row * a.V + (tok >= 0 && tok < a.V ? tok : 0)];
         while (base < n) {
             const int next = base + kLpStep, after = next + kLpStep;
-            if (next < n) load(v0, next);
-            later(v1, base);
-            if (next >= n) break;
-            if (after < n) load(v1, after);
-            later(v0, next);
+            if constexpr (!SMALL) load(v1, next);
+            trim(v0, base);
+            add(v0);
+            if constexpr (!SMALL) load(v0, after);
+            if (!SMALL && next < n) {
+                trim(v1, next);
+                add(v1);
+            }
             base = after;
         }
     }
@@ -313,9 +292,9 @@ __global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a)
         if (lane == 0) s_sums[wave] = u;
     }
     if (tid < kMaxTop) s_top[tid] = 0;
-    if (n_top > 0 && !one_step) {   // of the waves' candidates, those that reach the n_top-th largest of 64 groups
-        const float gm = across_quads(r.m, OpMax());
-        __syncthreads();   // the first thresholds have been read
+    const float mine = r.m;   // the largest of this thread's ids
+    if (n_top > 0) {
+        const float gm = across_quads(mine, OpMax());
         if ((lane & 3) == 0) s_group[tid >> 2] = gm;
     }
     __syncthreads();
@@ -323,24 +302,35 @@ __global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a)
 #pragma unroll
     for (int k = 1; k < kLpWaves; ++k) r = lp_join(r, s_sums[k], scale);
     if (n_top > 0) {
-        int most = 0;
-        if (!one_step) {
+        // the ids that reach the threshold: what the threads that have one read is read again, four ids a thread
+        const float least = fmaxf(nth_largest(s_group[lane], n_top), -3.402823466e38f);   // banned ids (-inf) are not taken
+        if (mine >= least) s_from[atomicAdd(&s_threads, 1)] = (uint8_t)tid;
+        __syncthreads();
+        const int items = s_threads << a.tiles_log << 2;   // each four ids
+#pragma unroll 1
+        for (int i = tid; i < items; i += kLpNT) {
+            const int t = s_from[i >> a.tiles_log >> 2], k = (i >> 2) & ((1 << a.tiles_log) - 1);
+            const int base = k * kLpStep + (t >> 6) * kLpTile, id = first(base) + 256 * (i & 3) + 4 * (t & 63);
+            if (base >= n) continue;
+            float v[4];
+            if constexpr (SMALL) {
 #pragma unroll
-            for (int k = 0; k < kLpWaves; ++k) most = max(most, s_count[k]);
-            if (most <= kLpCand) {
-                const uint32_t least = logit_key(nth_largest(s_group[lane], n_top));
-                for (int i = lane; i < s_count[wave]; i += 64) {
-                    const u64 k = cand[i];
-                    if ((uint32_t)(k >> 32) >= least) {
-                        const int p = atomicAdd(&s_left, 1);
-                        if (p < kLpFew) s_few[p] = k;
-                    }
-                }
+                for (int j = 0; j < 4; ++j) v[j] = id + j < n ? x[id + j] : -INFINITY;
+            } else {
+                const f32x4u_t u = *reinterpret_cast<const f32x4u_t*>(x + id);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = id + j >= base ? u[j] : -INFINITY;
             }
-            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (v[j] >= least) {
+                    const int p = atomicAdd(&s_left, 1);
+                    if (p < kLpFew) s_few[p] = id_key(v[j], lo + id + j);
+                }
         }
+        __syncthreads();
         const int left = s_left;
-        if (most <= kLpCand && left <= kLpFew && (left >= n_top || a.segs > 1)) rank_candidates(s_few, left, n_top, s_top);
+        if (left <= kLpFew && (left >= n_top || a.segs > 1)) rank_candidates(s_few, left, n_top, s_top);
         else one_by_one(x, n, lo);
         __syncthreads();
     }
@@ -418,7 +408,7 @@ static int logprob_segment(int M, int V, int n_top) {
     const long steps = (V + kLpStep - 1) / kLpStep;
     const long most = std::min<long>(kLpSegments, n_top > 0 ? kLpKeys / n_top : kLpSegments);
     const long segs = std::max<long>(1, std::min<long>({steps, most, kLpGrid / M}));
-    return (int)std::min<long>((steps + segs - 1) / segs * kLpStep, 0x7FFFF000);
+    return (int)((steps + segs - 1) / segs * kLpStep);
 }
 
 // Rows are cut while kLpGrid segments hold them all.
@@ -426,16 +416,18 @@ size_t logprob_part_bytes(int M, int V) { return V > kLpStep ? (size_t)std::min<
 
 hipError_t launch_token_logprobs(const float* logits, int M, int V, const int* tokens, float temperature, int n_top, float* lp,
                                  float* ent, int* ids, float* top_lp, void* part, int* counter, int* err, hipStream_t s) {
-    if (M < 1 || V < 1 || !(temperature > 0.f) || n_top < 0 || n_top > kMaxTop || n_top > V || (lp && !tokens) ||
+    if (M < 1 || V < 1 || V > (1 << 30) || !(temperature > 0.f) || n_top < 0 || n_top > kMaxTop || n_top > V || (lp && !tokens) ||
         (n_top && (!ids || !top_lp)))
         return hipErrorInvalidValue;
     const int seg = logprob_segment(M, V, n_top), segs = (int)(((long)V + seg - 1) / seg);
     if (segs > 1 && (!part || !counter)) return hipErrorInvalidValue;
     const int per = n_top > 0 ? std::min(n_top, 64 / segs) : 1;
+    int tiles_log = 0;
+    while (((long)kLpStep << tiles_log) < std::min(seg, V)) ++tiles_log;
     u64* sums = static_cast<u64*>(part);
-    LogprobArgs a{logits, M, V, segs, seg, tokens, 1.0f / temperature, n_top, lp, ent, ids, top_lp,
+    LogprobArgs a{logits, M, V, segs, seg, tokens, 1.0f / temperature, n_top, lp, ent, ids, top_lp, tiles_log,
                   sums, sums + (size_t)2 * M * segs, counter, per, (65536 + per - 1) / per, err};
-    hipLaunchKernelGGL(token_logprobs_kernel, dim3((unsigned)((size_t)M * segs)), dim3(kLpNT), 0, s, a);
+    hipLaunchKernelGGL(V < kLpTile ? token_logprobs_kernel<true> : token_logprobs_kernel<false>, dim3((unsigned)((size_t)M * segs)), dim3(kLpNT), 0, s, a);
     return hipGetLastError();
 }
 

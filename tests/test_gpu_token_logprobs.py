@@ -81,6 +81,20 @@ def test_many_rows():
     ctx.close()
 
 
+@pytest.mark.parametrize("V", [1024, 1025, 4095, 4097, 5121, 12289, 20483])
+@pytest.mark.parametrize("rows", [1, 1100])
+def test_ragged_tiles(V, rows):
+    """Rows cut into segments whose last is a few ids, and rows of one segment; the largest at both ends of the row and of
+    the last tiles."""
+    ctx = context(batch=1, q=rows, vocab=V)
+    x, tokens = logits(rows, V, V + rows, scale=1.0)
+    for i, at in enumerate((0, 1023, 1024, 4095, 4096, V - 1025, V - 1024, V - 5, V - 4, V - 1)):
+        if 0 <= at < V:
+            x[:, at] = 8.0 + i % 3
+    check(x, tokens, 1.0, 12, call(ctx, 1, rows, x, tokens, 1.0, 12))
+    ctx.close()
+
+
 @pytest.mark.parametrize("V,step", [(1000, 1.0), (9000, 8.0), (32016, 3.0), (32016, 0.0)])
 def test_ties_go_to_the_lower_id(V, step):
     ctx = context(batch=1, q=4, vocab=V)
@@ -212,7 +226,7 @@ def test_refusals():
     assert code(0, 3, x, tokens, 1.0, 0, f, f, None, None) == -1
     assert code(2, 3, None, tokens, 1.0, 0, f, f, None, None) == -1
     assert code(2, 3, x, None, 1.0, 0, f, f, None, None) == -1
-    for T in (0.0, -1.0, math.nan, math.inf):
+    for T in (0.0, -1.0, math.nan, math.inf, 1e-39):
         assert code(2, 3, x, tokens, T, 0, f, f, None, None) == -1
     assert code(2, 3, x, tokens, 1.0, -1, f, f, i, f) == -1
     assert code(2, 3, x, tokens, 1.0, 33, f, f, i, f) == -1
