@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kReorderMaxBatch) reorder_plan_kernel(int* cac
     __shared__ int s_wait[kReorderMaxBatch];     // of which are sources without a run
     __shared__ int s_at[kReorderMaxBatch];       // where its run begins, -1 without one
     __shared__ int s_op[kReorderMaxBatch], s_put[kReorderMaxBatch];
-    __shared__ int s_total, s_more;
+    __shared__ int s_total, s_more, s_end;
     const int b = threadIdx.x;
     int src = b;   // sequences from `batch` on stay
     int len = 0;
@@ -63,13 +63,14 @@ __global__ void __launch_bounds__(kReorderMaxBatch) reorder_plan_kernel(int* cac
         s_at[b] = -1;
         s_op[b] = RS_LOAD;
     }
-    if (b == 0) s_total = 0;
+    if (b == 0) s_total = s_end = 0;
     __syncthreads();
     const bool moves = b < all && src >= 0 && src != b;
     if (moves) atomicAdd(&s_dests[src], 1);
     __syncthreads();
     if (moves && s_dests[b] > 0) atomicAdd(&s_wait[src], 1);
     bool todo = b < all && s_dests[b] > 0;
+    if (todo) atomicMax(&s_end, (len + 31) / 32 * 32);
     for (;;) {
         __syncthreads();
         if (b == 0) s_more = 0;
@@ -97,7 +98,8 @@ __global__ void __launch_bounds__(kReorderMaxBatch) reorder_plan_kernel(int* cac
             s_op[c0] = RS_USE;
             total += 1 + s_dests[c0];
         }
-        *n_steps = total;
+        n_steps[0] = total;
+        n_steps[1] = s_end;
     }
     __syncthreads();
     if (b < all && s_dests[b] > 0) steps[s_at[b]] = int2{s_op[b] * 65536 + b, (len + 31) / 32 * 32};
@@ -105,9 +107,9 @@ __global__ void __launch_bounds__(kReorderMaxBatch) reorder_plan_kernel(int* cac
     if (b < batch) cache_len[b] = src < 0 ? 0 : s_len[src];
 }
 
-// The same list in one wave, a lane per sequence, left in LDS; returns its length.  src: the lane's (-1: none, lane
-// itself: stays), pages: its committed slots in whole pages.
-__device__ __forceinline__ int reorder_list(int src, int slots, int lane, int2* steps) {
+// The same list in one wave, a lane per sequence, left in LDS; returns its length and the longest source's slots.  src: the
+// lane's (-1: none, lane itself: stays), slots: its committed ones in whole pages.
+__device__ __forceinline__ int2 reorder_list(int src, int slots, int lane, int2* steps) {
     typedef unsigned long long u64;
     const bool moves = src >= 0 && src != lane;
     u64 dests = 0;   // of this lane as a source
@@ -154,29 +156,31 @@ __device__ __forceinline__ int reorder_list(int src, int slots, int lane, int2* 
     const u64 of = (u64)(uint32_t)__shfl((int)d_hi, s, 64) << 32 | (uint32_t)__shfl((int)d_lo, s, 64);
     const int base = __shfl(at, s, 64);
     if (moves) steps[base + 1 + __popcll(of & ((1ull << lane) - 1))] = int2{RS_STORE * 65536 + lane, 0};
-    return total;
+    return int2{total, (int)across_wave(dests ? (float)slots : 0.f, OpMax())};   // exact: capacities are below 2^24
 }
 
 struct ReorderArgs {
     u32x4_t* kc; u32x4_t* vc;
     size_t layer_cells, head_cells;    // 16-byte cells of a layer's K (or V), of a sequence's head
-    int n_layers, batch, all, H, S_max, slot_cells, first, chunks;
+    int n_layers, batch, all, H, S_max, slot_cells, first;
     int* cache_len; const int* src;
-    const int2* steps; const int* n_steps;   // made ahead (more than 64 sequences)
+    const int2* steps; const int* n_steps;   // made ahead: the list, its length and the longest source's slots
     int* arrived; int* err;
 };
 
-// Chunks of 256 * kReorderCells cells of the pages from `first` on, of each layer, K and V, and head.
+// Chunks of 256 * kReorderCells cells of the pages from `first` on, of each layer, K and V, and head.  The host's grid holds
+// them all as far as it knows the lengths; workgroups take further ones where the device's are longer (a replayed graph).
 static constexpr int kReorderCells = 2, kReorderAlone = 8192;   // cells per thread; workgroups that make the list themselves, at most
 template <bool AHEAD>
 __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderArgs a) {
     __shared__ int2 s_steps[AHEAD ? 1 : 3 * 64];
-    __shared__ int s_n;
+    __shared__ int2 s_n;
     const int2* steps = a.steps;
-    int n, now = 0;
+    int2 made;
+    int now = 0;
     bool wrong = false;   // wave 0: the lane's new length, and whether its source is out of range
     if constexpr (AHEAD) {
-        n = *a.n_steps;
+        made = int2{a.n_steps[0], a.n_steps[1]};
     } else {
         if (threadIdx.x < 64) {
             const int lane = threadIdx.x;
@@ -184,20 +188,22 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderArgs a) {
             const int len = lane < a.all ? min(max(a.cache_len[lane], 0), a.S_max) : 0;
             const bool bad = lane < a.batch && (src < -1 || src >= a.all);
             if (bad) src = lane;
-            const int total = reorder_list(src, (len + 31) / 32 * 32, lane, s_steps);
-            if (lane == 0) s_n = total;
+            const int2 list = reorder_list(src, (len + 31) / 32 * 32, lane, s_steps);
+            if (lane == 0) s_n = list;
             now = __shfl(len, max(src, 0), 64);
             if (src < 0) now = 0;
             wrong = bad;
         }
         __syncthreads();
-        n = s_n;
+        made = s_n;
         steps = s_steps;
     }
-    const int items = n == 0 ? 0 : a.chunks * 2 * a.H * a.n_layers;
+    const int n = __builtin_amdgcn_readfirstlane(made.x), end_slot = __builtin_amdgcn_readfirstlane(made.y);
+    const uint32_t chunks = (uint32_t)(((size_t)max(0, end_slot - a.first) * a.slot_cells + 256 * kReorderCells - 1) / (256 * kReorderCells));
+    const size_t items = (size_t)chunks * 2 * a.H * a.n_layers;
     const size_t seq_cells = (size_t)a.H * a.head_cells;
-    if (const int item = blockIdx.x; item < items) {
-        const int chunk = item % a.chunks, y = item / a.chunks % (2 * a.H), layer = item / a.chunks / (2 * a.H);
+    for (size_t at = blockIdx.x; at < items; at += gridDim.x) {
+        const uint32_t item = (uint32_t)at, chunk = item % chunks, of = item / chunks, y = of % (2 * a.H), layer = of / (2 * a.H);
         u32x4_t* base = (y & 1 ? a.vc : a.kc) + layer * a.layer_cells + (y >> 1) * a.head_cells;
         size_t cell[kReorderCells];
 #pragma unroll
@@ -264,7 +270,8 @@ hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n
     const int slot_cells = Dh * esz / 16;
     const size_t cells = (size_t)std::max(0, end - first) * slot_cells;
     const long chunks = (long)((cells + 256 * kReorderCells - 1) / (256 * kReorderCells)), items = chunks * 2 * H * n_layers;
-    if (items > 0x7FFFFFFF) return hipErrorInvalidValue;
+    const long most = ((long)S_max * slot_cells + 256 * kReorderCells - 1) / (256 * kReorderCells) * 2 * H * n_layers;
+    if (most > 0x7FFFFFFF || S_max >= 1 << 24) return hipErrorInvalidValue;
     const bool ahead = all > 64 || items > kReorderAlone;
     if (ahead) {
         hipLaunchKernelGGL(reorder_plan_kernel, dim3(1), dim3((all + 63) / 64 * 64), 0, s, cache_len, batch, all, S_max, src,
@@ -272,12 +279,10 @@ hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (items == 0 && ahead) return hipSuccess;   // no page to move
     ReorderArgs a{};
     a.kc = static_cast<u32x4_t*>(kc); a.vc = static_cast<u32x4_t*>(vc);
     a.layer_cells = layer_elems * esz / 16; a.head_cells = (size_t)S_max * slot_cells;
     a.n_layers = n_layers; a.batch = batch; a.all = all; a.H = H; a.S_max = S_max; a.slot_cells = slot_cells; a.first = first;
-    a.chunks = (int)chunks;
     a.cache_len = cache_len; a.src = src; a.steps = reinterpret_cast<const int2*>(steps + kReorderHead);
     a.n_steps = steps + kReorderHead - 2;
     a.arrived = steps; a.err = err;

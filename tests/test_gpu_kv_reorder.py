@@ -167,3 +167,26 @@ def test_captured_on_a_stream_of_its_own():
             assert length.tolist() == want[2] and torch.equal(k.cpu(), want[0]) and torch.equal(v.cpu(), want[1])
             check(ctx, lens, [3, 3, 1, 2], 32, seed=20 + i)   # the program's own calls between replays
     ctx.close()
+
+
+@pytest.mark.parametrize("batch,slots,short", [(4, 300, 3), (4, 300, 0), (70, 96, 1), (70, 96, 0)])
+def test_a_graph_captured_for_shorter_sequences(batch, slots, short):
+    """The lengths grow on the device between replays: every committed page moves."""
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ctx = context(2, 64, "bf16", layers=2, batch=batch, slots=slots)
+        src = torch.arange(batch, dtype=torch.int32, device="cuda").roll(1)
+        fill(ctx, [short] * batch, 1)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            B.sdsat_kv_reorder(ctx.handle, batch, src, 32)
+        for i in range(3):
+            lens = [(slots * (b + 1 + i)) % (slots + 1) for b in range(batch)]
+            k, v, length = fill(ctx, lens, 10 + i)
+            want = expected(k.cpu(), v.cpu(), lens, src.tolist(), 32)
+            graph.replay()
+            s.synchronize()
+            assert length.tolist() == want[2] and torch.equal(k.cpu(), want[0]) and torch.equal(v.cpu(), want[1])
+            check(ctx, lens, src.tolist(), 0, seed=20 + i)   # the program's own calls between replays
+    ctx.close()
