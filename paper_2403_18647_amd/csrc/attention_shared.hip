@@ -634,10 +634,11 @@ __global__ void __launch_bounds__(256, STAGED || sizeof(T) * DH > 256 ? 2 : 3) s
     }
     const int tiles = (a.at.q + 15) / 16, i = (int)blockIdx.x - a.prefix_grid, part = i % a.own_parts, j = i / a.own_parts;
     const OwnRows o = own_rows(a, j / tiles, j % tiles, 16);
-    const int lo = o.pages + part * a.own_chunk;
+    // the last part takes what is left: the device's lengths may exceed the host's (a replayed graph)
+    const int lo = o.pages + part * a.own_chunk, most = a.at.S_max / 32, end = part == a.own_parts - 1 ? most : min(lo + a.own_chunk, most);
     WaveAttention<T, DH, 1> w;
-    attend_few<T, DH, kOwnLanes>(w, a.at, head_cache<T, DH>(a.at, o.b, o.b, o.h, 0), lo, min(lo + a.own_chunk, a.at.S_max / 32),
-                                 o.row0, o.rows, o.h, o.m0, wave, lane, a.at.cache_len + o.b, [&](int L, int& hi) {
+    attend_few<T, DH, kOwnLanes>(w, a.at, head_cache<T, DH>(a.at, o.b, o.b, o.h, 0), lo, end, o.row0, o.rows, o.h, o.m0, wave,
+                                 lane, a.at.cache_len + o.b, [&](int L, int& hi) {
         if (part == 0) report(a, L, o.pages);
         hi = min(hi, key_blocks(a, L, a.at.q));
         return own_sight(a, o.b, L);

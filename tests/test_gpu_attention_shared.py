@@ -299,3 +299,28 @@ def test_captured_on_a_stream_of_its_own(q):
             check(replayed, ref, tol)
             assert torch.equal(run(ctx, 3, prefix, q, x), replayed)
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype,dh,q", [("bf16", 128, 3), ("fp32", 64, 3), ("bf16", 64, 70)])
+def test_a_graph_captured_for_shorter_sequences(dtype, dh, q):
+    """The lengths grow on the device between replays: every committed slot counts."""
+    prefix, own = [70], [2100, 1500]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ctx, keys, vals, x = case(dtype, 2, dh, 2, prefix, own, q, slots=4000)
+        out = torch.full_like(x, 7e7)
+        B.sdsat_set_cache_len(ctx.handle, [75, 71])
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            B.sdsat_attention_shared(ctx.handle, 0, 2, q, 2, prefix, x, None, out)
+        B.sdsat_set_cache_len(ctx.handle, [prefix[0] + n for n in own])
+        ref, tol = reference(keys, vals, x, q, chain(keys, q))
+        for _ in range(2):
+            out.fill_(7e7)
+            graph.replay()
+            s.synchronize()
+            check(out, ref, tol)
+            run(ctx, 2, prefix, q, x)
+        assert device_error(ctx) == 0
+    ctx.close()
