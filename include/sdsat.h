@@ -174,7 +174,7 @@ int sdsat_verify_nucleus(sdsat_ctx* ctx, int32_t batch, int32_t q, const float* 
                          int32_t* d_n_accept);
 
 /* Log probabilities for ranking and reporting completions.  For each logits row
- * (b, j) of [batch*q, V] float32, with z = logits / temperature (> 0, finite):
+ * (b, j) of [batch*q, V] float32, with z = logits / temperature (> 0, finite, as is 1 / temperature):
  *   d_logprob[b*q + j]  log softmax(z)[d_tokens[b*q + j]]; 0 where the token is
  *                       negative (a row without one); a token >= V gives NaN
  *                       and SDSAT_EDATA at the next synchronous call;
