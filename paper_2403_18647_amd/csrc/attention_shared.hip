@@ -25,15 +25,24 @@
 // (rows in lanes, keys in registers and lane groups), and O^T += V^T P^T takes P
 // as it stands.  Two kinds of workgroup do this, with the same values:
 //  * few rows, and float models: a wave per key lane and 16 rows, K and V
-//    straight from the cache into registers; bound by HBM;
+//    straight from the cache into registers; bound by HBM: two groups of 8
+//    sequences, one row each over 2011 shared and 300 own slots of 32 heads of 128
+//    (119 MB) 31 us, 3.8 TB/s (a read stream 6.3); a second launch, the join, 4.5 of it;
 //  * many rows of bf16 models: 64 rows, two key lanes of two waves with 32 rows
 //    each; the blocks go straight into LDS while the ones before are used, Q
-//    stays in registers; bound by the matrix cores.
-// On bf16 models Q and P enter the matrix cores as value and remainder, so that
-// float accuracy is kept.  Scores are in units of log 2 (the scale is folded
-// into Q) and a row's maximum is only raised when a score exceeds it by more
-// than kRaise: the weights then stay below 2^kRaise, exact in float, and most
-// blocks need no rescaling of O and no exchange between lanes.
+//    stays in registers; bound by the matrix cores and by what a block's steps wait
+//    for each other: 16 sequences of 11 rows over 16384 shared and 400 own slots of
+//    40 heads of 128 (121 GFLOP with the remainders) 155 us; 8 blocks of 128 rows
+//    over 4000 slots (136 GFLOP) 128 us, 1.07 PFLOP/s (a large product 1.19); two
+//    workgroups a CU, so 4 such blocks take 110 us.
+// On bf16 models Q and P enter the matrix cores as value and remainder, as in
+// attention.hip: 16 bits of each, outputs within 3.5e-6 of their size of the
+// 64-bit result (float32 arithmetic 0.7e-6 to 2.3e-6); a third term would add
+// half as many products again, and the many-row kernel is bound by them.
+// Scores are in units of log 2 (the scale is folded into Q) and a row's maximum
+// is only raised when a score exceeds it by more than kRaise: the weights then
+// stay below 2^kRaise, far from the end of float's range, and most blocks need
+// no rescaling of O and no exchange between lanes.
 //
 // Key ranges depend on the prefix lengths, the number of sequences and the cache
 // capacity, never on q: a row's result is bitwise the same in blocks of any
@@ -694,7 +703,11 @@ __global__ void __launch_bounds__(256, 2) shared_rows_kernel(SharedArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     constexpr int TILE = sizeof(T) == 2 ? kTileRows : 16;
     __shared__ __align__(1024) unsigned char smem[sizeof(T) == 2 ? TileShape<DH>::BYTES : FewBytes<DH>];
-    const OwnRows o = own_rows(a, (int)blockIdx.x / a.tiles, a.tiles - 1 - (int)blockIdx.x % a.tiles, TILE);
+    // a ragged last tile of few rows after the others, beside which it fits; a head's tiles on one XCD where heads come in
+    // eights
+    const int nth = (int)blockIdx.x / (a.at.B * a.at.H), last = a.at.q % TILE;
+    const int tile = last && 2 * last <= TILE ? (nth + 1 == a.tiles ? nth : a.tiles - 2 - nth) : a.tiles - 1 - nth;
+    const OwnRows o = own_rows(a, (int)blockIdx.x % (a.at.B * a.at.H), tile, TILE);
     const int L = __builtin_amdgcn_readfirstlane(a.at.cache_len[o.b]), nblk = key_blocks(a, L, o.m0 + TILE);   // what the tile's last row can see
     report(a, L, o.pages);
     const Sight see = own_sight(a, o.b, L);
