@@ -179,8 +179,10 @@ struct WaveAttention {
         bool rise = false;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            lm[t] = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])),
-                          fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
+            // the larger of two as a median: fmaxf would first quiet each product sum, an instruction more
+            auto larger = [](float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); };
+            lm[t] = larger(larger(larger(s[t][0][0], s[t][0][1]), larger(s[t][0][2], s[t][0][3])),
+                           larger(larger(s[t][1][0], s[t][1][1]), larger(s[t][1][2], s[t][1][3])));
             rise |= lm[t] > rmax[t] + kRaise;
         }
         if (__any(rise)) {
@@ -438,8 +440,10 @@ __device__ __forceinline__ void tile_step(WaveAttention<uint16_t, DH, 2>& w, uns
         if (dt + 2 < NDT) v_frags(f[(NDS + dt / 2 + 1) & 1], dt + 2);
         __builtin_amdgcn_sched_barrier(0);
         if (junk) {
+            int key0 = 32 * blk;
+            asm volatile("" : "+v"(key0));   // the masks are made here, in the last block, not in every one
 #pragma unroll
-            for (int u = 0; u < 2; ++u) drop_keys<T>(vf[u], 32 * blk, g, see.Tb);
+            for (int u = 0; u < 2; ++u) drop_keys<T>(vf[u], key0, g, see.Tb);
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u)
