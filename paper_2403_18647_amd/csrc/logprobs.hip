@@ -14,7 +14,7 @@
 // streams each.  Its threads keep their own running maximum, sum and weighted
 // sum (no exchange while data arrives) and join them at the end.  For the n_top
 // largest, the threads' maxima serve: at least n_top ids reach the n_top-th
-// largest maximum of 64 groups of 4 threads, so only ids that do are candidates,
+// largest maximum of 64 groups of threads, so only ids that do are candidates,
 // little more than n_top for logits in no order, and only threads whose own
 // maximum does have any.  The workgroup reads those threads' ids once more (from
 // a cache), gathers the candidates in LDS as 64-bit keys (the logit as an
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a)
     __shared__ u64 s_cand[kLpKeys];
     __shared__ u64 s_top[kMaxTop], s_key[kLpWaves];   // the largest keys, in order
     __shared__ u64 s_few[kLpFew];
-    __shared__ float s_group[64];
+    __shared__ float s_group[kLpWaves][64];
     __shared__ LpSums s_sums[kLpWaves];
     __shared__ uint8_t s_from[kLpNT];
     __shared__ int s_threads, s_left, s_last;
@@ -294,8 +294,7 @@ __global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a)
     if (tid < kMaxTop) s_top[tid] = 0;
     const float mine = r.m;   // the largest of this thread's ids
     if (n_top > 0) {
-        const float gm = across_quads(mine, OpMax());
-        if ((lane & 3) == 0) s_group[tid >> 2] = gm;
+        s_group[wave][lane] = mine;   // groups across the waves: a short row lies in the first one
     }
     __syncthreads();
     r = s_sums[0];
@@ -303,7 +302,10 @@ __global__ void __launch_bounds__(kLpNT, 7) token_logprobs_kernel(LogprobArgs a)
     for (int k = 1; k < kLpWaves; ++k) r = lp_join(r, s_sums[k], scale);
     if (n_top > 0) {
         // the ids that reach the threshold: what the threads that have one read is read again, four ids a thread
-        const float least = fmaxf(nth_largest(s_group[lane], n_top), -3.402823466e38f);   // banned ids (-inf) are not taken
+        float group = s_group[0][lane];
+#pragma unroll
+        for (int k = 1; k < kLpWaves; ++k) group = fmaxf(group, s_group[k][lane]);
+        const float least = fmaxf(nth_largest(group, n_top), -3.402823466e38f);   // banned ids (-inf) are not taken
         if (mine >= least) s_from[atomicAdd(&s_threads, 1)] = (uint8_t)tid;
         __syncthreads();
         const int items = s_threads << a.tiles_log << 2;   // each four ids
