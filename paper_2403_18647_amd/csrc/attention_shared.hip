@@ -33,7 +33,7 @@
 //    stays in registers; bound by the matrix cores and by what a block's steps wait
 //    for each other: 16 sequences of 11 rows over 16384 shared and 400 own slots of
 //    40 heads of 128 (121 GFLOP with the remainders) 155 us; 8 blocks of 128 rows
-//    over 4000 slots (136 GFLOP) 128 us, 1.07 PFLOP/s (a large product 1.19); two
+//    over 4000 slots (136 GFLOP) 124 us, 1.10 PFLOP/s (a large product 1.19); two
 //    workgroups a CU, so 4 such blocks take 110 us.
 // On bf16 models Q and P enter the matrix cores as value and remainder, as in
 // attention.hip: 16 bits of each, outputs within 3.5e-6 of their size of the
