@@ -143,7 +143,8 @@ int sdsat_forward_block(sdsat_ctx* ctx, int32_t batch, int32_t q, const int32_t*
  * knows).  Outputs, masks and the tentative K and V as sdsat_forward_block; a
  * row's attention is summed in another order than there, the same for every
  * block of up to 64 rows per sequence.  group 1 is sdsat_forward_block.
- * Stream-ordered; h_prefix_len is read during the call. */
+ * A head's K of one sequence (max_ctx * head_dim elements) must stay below
+ * 4 GiB.  Stream-ordered; h_prefix_len is read during the call. */
 int sdsat_forward_block_shared(sdsat_ctx* ctx, int32_t batch, int32_t q, int32_t group,
                                const int32_t* h_prefix_len, const int32_t* d_tokens,
                                const uint64_t* d_ancestor_mask, float* d_logits);
@@ -211,7 +212,8 @@ int sdsat_commit_kv(sdsat_ctx* ctx, int32_t batch, int32_t q, const int32_t* d_n
  * that holds first_slot to the last with a committed slot of the source; the
  * ones before are left as they are (a prefix that the sequences share or all
  * hold).  Slots past cache_len are unspecified afterwards (a block's tentative
- * rows do not move).  In place; needs max_batch <= 1024.  Stream-ordered. */
+ * rows do not move).  In place; needs max_batch <= 1024 and max_ctx below 2^24.
+ * Stream-ordered. */
 int sdsat_kv_reorder(sdsat_ctx* ctx, int32_t batch, const int32_t* d_src, int32_t first_slot);
 
 /* Device pointers to one layer of the cache in the configuration's type, for

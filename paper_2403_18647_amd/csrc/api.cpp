@@ -556,6 +556,8 @@ int check_share(sdsat_ctx* c, int B, int group, const int32_t* h_prefix_len, Sha
     if (group < 1 || B % group) return fail(c, SDSAT_EINVAL, "batch must be a multiple of group");
     if (B / group > kMaxShareGroups) return fail(c, SDSAT_EUNSUPPORTED, "at most 64 groups share prefixes in one call");
     if (!h_prefix_len) return fail(c, SDSAT_EINVAL, "h_prefix_len is NULL");
+    if (group > 1 && !shared_supported(c->D.S, c->D.Dh, c->D.esz))
+        return fail(c, SDSAT_EUNSUPPORTED, "a head's cache of one sequence is too large to share");
     share->group = group;
     for (int g = 0; g < B / group; ++g) {
         if (h_prefix_len[g] < 0) return fail(c, SDSAT_EINVAL, "negative prefix length");
@@ -834,7 +836,8 @@ int sdsat_kv_reorder(sdsat_ctx* c, int32_t batch, const int32_t* d_src, int32_t 
     const DeviceScope scope(c->device);
     const Dims& D = c->D;
     if (batch < 1 || batch > D.maxB) return fail(c, SDSAT_EINVAL, "batch out of range");
-    if (D.maxB > kReorderMaxBatch) return fail(c, SDSAT_EUNSUPPORTED, "reordering needs max_batch <= 1024");
+    if (!reorder_supported(D.esz, D.maxB, D.L, D.H, D.Dh, D.S))
+        return fail(c, SDSAT_EUNSUPPORTED, "reordering needs max_batch <= 1024 and max_ctx below 2^24");
     if (!d_src) return fail(c, SDSAT_EINVAL, "d_src is NULL");
     if (first_slot < 0 || first_slot > D.S) return fail(c, SDSAT_EINVAL, "first_slot out of range");
     const int most = max_hint(c, D.maxB);

@@ -752,7 +752,8 @@ hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p,
                                    hipEvent_t ev1) {
     const AttnArgs& at = a.at;
     if (at.q < 1 || at.q > 4096 || (at.mask && at.q > 64) || at.B < 1 || at.H < 1 || a.group < 1 || at.B % a.group ||
-        at.B / a.group > kMaxShareGroups || at.S_max < 32 || at.S_max % 32 || at.ldo % 4 || !at.qbuf || !at.kc || !at.vc ||
+        at.B / a.group > kMaxShareGroups || at.S_max < 32 || at.S_max % 32 || !shared_supported(at.S_max, head_dim, dtype == 1 ? 2 : 4) ||
+         at.ldo % 4 || !at.qbuf || !at.kc || !at.vc ||
         !at.cache_len || !at.out || !at.err || p.whole != (at.q > kAttnSplitRows) || (!p.whole && !a.part) ||
         (dtype != 1 && p.staged) || (dtype == 1 && p.whole && !p.staged))
         return hipErrorInvalidValue;

@@ -165,6 +165,8 @@ struct SharedPlan {
     // pages of a prefix part, parts; pages of an own part, parts; parts of a row; row tiles; workgroups of the prefix, of all
     int chunk, prefix_parts, own_chunk, own_parts, slots, tiles, prefix_grid, grid;
 };
+// the kernels address a head's K (or V) of one sequence by 32-bit byte offsets
+inline bool shared_supported(int S_max, int head_dim, int esz) { return (size_t)S_max * head_dim * esz <= 0xFFF00000u; }
 SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pages, int max_len, int S_max);
 size_t shared_partial_floats(const SharedPlan& p, int B, int q, int H, int head_dim);
 size_t shared_partial_floats_most(int B_max, int H, int q_max, int head_dim);
@@ -176,6 +178,7 @@ hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p,
 // up to max_len at the most, and the lengths.  steps: kReorderHead ints, zero between launches (arrival counts, a cache
 // line each), and 6 * all
 constexpr int kReorderMaxBatch = 1024, kReorderCounts = 16, kReorderHead = 32 * (1 + kReorderCounts) + 32;
+bool reorder_supported(int esz, int all, int n_layers, int H, int Dh, int S_max);
 hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n_layers, int batch, int all, int H, int Dh,
                           int S_max, int* cache_len, int max_len, const int* src, int first_slot, int* steps, int* err,
                           hipStream_t s);

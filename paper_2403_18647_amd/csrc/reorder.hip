@@ -260,6 +260,12 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderArgs a) {
     }
 }
 
+// Sequences that one workgroup's threads hold, slots that a float holds, chunks that a grid holds.
+bool reorder_supported(int esz, int all, int n_layers, int H, int Dh, int S_max) {
+    const long cells = (long)S_max * (Dh * esz / 16), most = (cells + 256 * kReorderCells - 1) / (256 * kReorderCells) * 2 * H * n_layers;
+    return all <= kReorderMaxBatch && S_max < 1 << 24 && most <= 0x7FFFFFFF;
+}
+
 hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n_layers, int batch, int all, int H, int Dh,
                           int S_max, int* cache_len, int max_len, const int* src, int first_slot, int* steps, int* err,
                           hipStream_t s) {
@@ -270,8 +276,7 @@ hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n
     const int slot_cells = Dh * esz / 16;
     const size_t cells = (size_t)std::max(0, end - first) * slot_cells;
     const long chunks = (long)((cells + 256 * kReorderCells - 1) / (256 * kReorderCells)), items = chunks * 2 * H * n_layers;
-    const long most = ((long)S_max * slot_cells + 256 * kReorderCells - 1) / (256 * kReorderCells) * 2 * H * n_layers;
-    if (most > 0x7FFFFFFF || S_max >= 1 << 24) return hipErrorInvalidValue;
+    if (!reorder_supported(esz, all, n_layers, H, Dh, S_max)) return hipErrorInvalidValue;
     const bool ahead = all > 64 || items > kReorderAlone;
     if (ahead) {
         hipLaunchKernelGGL(reorder_plan_kernel, dim3(1), dim3((all + 63) / 64 * 64), 0, s, cache_len, batch, all, S_max, src,

@@ -89,6 +89,7 @@ int main() {
         a = args(6); a.pages[0] = p.chunk * p.prefix_parts + 1; bad("pages without a part", 1, 64, a, p);
         a = args(6); a.part = nullptr; bad("no buffer for the parts", 1, 64, a, p);
         a = args(6); a.at.S_max = 250; bad("a cache of broken pages", 1, 64, a, p);
+        a = args(6); a.at.S_max = 1 << 25; bad("4 GiB of keys of a head", 1, 64, a, p);
         a = args(6); a.at.ldo = 130; bad("an odd row stride", 1, 64, a, p);
         a = args(6); a.at.qbuf = nullptr; bad("no queries", 1, 64, a, p);
         a = args(65); bad("a decode plan for a long block", 1, 64, a, p);
@@ -109,6 +110,7 @@ int main() {
         bad("broken pages", 2, 4, 4, 64, 120, 20, dummy, 0);
         bad("a length past the slots", 2, 4, 4, 64, 128, 129, dummy, 0);
         bad("a negative slot", 2, 4, 4, 64, 128, 20, dummy, -1);
+        bad("2^24 slots", 2, 4, 4, 64, 1 << 24, 20, dummy, 0);
         bad("no map", 2, 4, 4, 64, 128, 20, nullptr, 0);
         bad("rows of 8 bytes", 2, 4, 4, 4, 128, 20, dummy, 0);
     }
