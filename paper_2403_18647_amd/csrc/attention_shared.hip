@@ -411,11 +411,19 @@ __device__ __forceinline__ void tile_step(WaveAttention<uint16_t, DH, 2>& w, uns
         for (int u = 0; u < 2; ++u)
             vf[u] = Frag<T>::load(reinterpret_cast<const T*>(stage + S::HALF + (dt + u) * 1024 + lane * 16));
     };
+    // While loads into LDS are in flight the compiler waits for every read of LDS where it needs one: what a group needs is
+    // waited for here, before the next one's reads are issued
+    auto landed = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt 0
+        __builtin_amdgcn_sched_barrier(0);
+    };
     Frag<T> f[2][2];
     k_frags(f[0], 0);
 #pragma unroll
     for (int ds = 0; ds < NDS; ++ds) {
         const Frag<T> (&kf)[2] = f[ds & 1];
+        landed();
         if (ds + 1 < NDS) k_frags(f[(ds + 1) & 1], ds + 1);
         else v_frags(f[(ds + 1) & 1], 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -437,6 +445,7 @@ __device__ __forceinline__ void tile_step(WaveAttention<uint16_t, DH, 2>& w, uns
 #pragma unroll
     for (int dt = 0; dt < NDT; dt += 2) {
         Frag<T> (&vf)[2] = f[(NDS + dt / 2) & 1];
+        landed();
         if (dt + 2 < NDT) v_frags(f[(NDS + dt / 2 + 1) & 1], dt + 2);
         __builtin_amdgcn_sched_barrier(0);
         if (junk) {
