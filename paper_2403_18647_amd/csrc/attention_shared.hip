@@ -175,12 +175,14 @@ struct WaveAttention {
                 }
             }
         }
-        float lm[RT];
+        // the larger of two as the median with infinity (that the compiler cannot see): fmaxf would first quiet each product
+        // sum, an instruction more
+        float lm[RT], inf = INFINITY;
+        asm("" : "+s"(inf));
         bool rise = false;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            // the larger of two as a median: fmaxf would first quiet each product sum, an instruction more
-            auto larger = [](float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); };
+            auto larger = [&](float a, float b) { return __builtin_amdgcn_fmed3f(a, b, inf); };
             lm[t] = larger(larger(larger(s[t][0][0], s[t][0][1]), larger(s[t][0][2], s[t][0][3])),
                            larger(larger(s[t][1][0], s[t][1][1]), larger(s[t][1][2], s[t][1][3])));
             rise |= lm[t] > rmax[t] + kRaise;
