@@ -324,3 +324,34 @@ def test_a_graph_captured_for_shorter_sequences(dtype, dh, q):
             run(ctx, 2, prefix, q, x)
         assert device_error(ctx) == 0
     ctx.close()
+
+
+def test_caches_past_32_bit_offsets():
+    """The last group's keys lie more than 4 GiB into the layer; the other sequences hold nothing but their block's row."""
+    heads, dh, batch, prefix, own = 40, 128, 16, 32700, [40, 7]
+    ctx = context(heads, dh, "bf16", 1, batch, 32768, 1)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    k, v, _ = ctx.cache()
+    assert k[0, 14].storage_offset() * 2 - k.storage_offset() * 2 > 2 ** 32
+    keys, vals = [], []
+    for b in (14, 15):
+        total = prefix + own[b - 14] + 1
+        mine = [torch.randn((heads, total, dh), generator=g, device="cuda").bfloat16() for _ in range(2)]
+        if b == 15:
+            for t, o in zip(mine, (keys, vals)):
+                t[:, :prefix] = o[0][:, :prefix].bfloat16()
+        lo = prefix // 32 * 32 if b == 15 else 0
+        flat = torch.zeros((heads, 32768, dh), dtype=torch.bfloat16, device="cuda")
+        flat[:, lo:total] = mine[1][:, lo:]
+        k[0, b, :, lo:total] = mine[0][:, lo:]
+        v[0, b].copy_(flat.view(v[0, b].shape))
+        keys.append(mine[0].double())
+        vals.append(mine[1].double())
+    B.sdsat_set_cache_len(ctx.handle, [0] * 14 + [prefix + n for n in own])
+    x = torch.randn((batch, heads * dh), generator=g, device="cuda")
+    out = run(ctx, 2, [0] * 7 + [prefix], 1, x)
+    ref, tol = reference(keys, vals, x[14:], 1, chain(keys, 1))
+    check(out[14:], ref, tol)
+    assert not out[:14].any()   # their one key's V is zero
+    ctx.close()

@@ -190,3 +190,26 @@ def test_a_graph_captured_for_shorter_sequences(batch, slots, short):
             assert length.tolist() == want[2] and torch.equal(k.cpu(), want[0]) and torch.equal(v.cpu(), want[1])
             check(ctx, lens, src.tolist(), 0, seed=20 + i)   # the program's own calls between replays
     ctx.close()
+
+
+def test_caches_past_32_bit_offsets():
+    """Sequences that lie more than 4 GiB into the layer change places with the first ones."""
+    ctx = context(40, 128, "bf16", layers=1, batch=16, slots=32768)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    k, v, length = ctx.cache()
+    lens = {0: 31000, 1: 5, 14: 32768, 15: 100}
+    for b in lens:
+        k[0, b] = torch.randn(k[0, b].shape, generator=g, device="cuda")
+        v[0, b] = torch.randn(v[0, b].shape, generator=g, device="cuda")
+    old = {b: (k[0, b].clone(), v[0, b].clone()) for b in lens}
+    B.sdsat_set_cache_len(ctx.handle, [lens.get(b, 0) for b in range(16)])
+    src = list(range(16))
+    src[0], src[1], src[14], src[15] = 14, 15, 0, 14
+    B.sdsat_kv_reorder(ctx.handle, 16, torch.tensor(src, dtype=torch.int32, device="cuda"), 0)
+    torch.cuda.synchronize()
+    for b, a in ((0, 14), (1, 15), (14, 0), (15, 14)):
+        n = -(-lens[a] // 32)
+        assert int(length[b]) == lens[a]
+        assert torch.equal(k[0, b, :, :32 * n], old[a][0][:, :32 * n]) and torch.equal(v[0, b, :, :n], old[a][1][:, :n])
+    ctx.close()
