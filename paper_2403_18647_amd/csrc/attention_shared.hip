@@ -40,10 +40,12 @@
 // attention.hip: 16 bits of each, outputs within 3.5e-6 of their size of the
 // 64-bit result (float32 arithmetic 0.7e-6 to 2.3e-6); a third term would add
 // half as many products again, and the many-row kernel is bound by them.
-// Scores are in units of log 2 (the scale is folded into Q) and a row's maximum
-// is only raised when a score exceeds it by more than kRaise: the weights then
-// stay below 2^kRaise, far from the end of float's range, and most blocks need
-// no rescaling of O and no exchange between lanes.
+// Scores are in units of log 2 (the scale is folded into Q).  A row keeps a base,
+// and its products are added to minus the base, so that the weights are 2 to what
+// comes out.  The base begins at the maximum of the row's first block and is only
+// raised, to the maximum at hand, when a score exceeds it by more than kRaise: the
+// weights stay below 2^kRaise, far from the end of float's range, and most blocks
+// need no rescaling of O and no exchange between lanes.
 //
 // Key ranges depend on the prefix lengths, the number of sequences and the cache
 // capacity, never on q: a row's result is bitwise the same in blocks of any
@@ -142,23 +144,25 @@ __device__ __forceinline__ void drop_keys(Frag<T>& f, int key0, int g, int Tb) {
 struct Sight { int L, Tb, q; const uint64_t* mask; };
 
 // One wave's share of an attention over 32-key blocks: RT 16-row tiles of queries, the scores of the block at hand, and
-// the running maxima, sums and weighted V of each row (row tile t's column c is row 16 t + c).
+// the bases, sums and weighted V of each row (row tile t's column c is row 16 t + c).
 template <typename T, int DH, int RT>
 struct WaveAttention {
     static constexpr int NDT = DH / 16;
-    f32x4_t s[RT][2], o[RT][NDT];   // s[t][kt][r] = S^T[key 16 kt + 4 g + r][row 16 t + c]
-    float rmax[RT], rsum[RT];
+    f32x4_t s[RT][2], o[RT][NDT];   // s[t][kt][r] = S^T[key 16 kt + 4 g + r][row 16 t + c] less the row's base
+    f32x4_t minus[RT];              // minus the row's base (0 before its first key): what the products are added to
+    float rise[RT], rsum[RT];       // scores above it raise the base: kRaise, or -inf before the first key
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            rmax[t] = -INFINITY;
+            minus[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            rise[t] = -INFINITY;
             rsum[t] = 0.f;
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) o[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // The scores of block blk as its rows see them, and the maxima raised where they have to be.  m0: block row of tile 0.
+    // The scores of block blk as its rows see them, and the bases raised where they have to be.  m0: block row of tile 0.
     __device__ __forceinline__ void look(int blk, int m0, const Sight& see, int lane) {
         const int c = lane & 15, g = lane >> 4;
         if (32 * blk + 32 > see.L) {
@@ -180,35 +184,40 @@ struct WaveAttention {
         // sum, an instruction more
         float lm[RT], inf = INFINITY;
         asm("" : "+s"(inf));
-        bool rise = false;
+        bool any = false;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             auto larger = [&](float a, float b) { return __builtin_amdgcn_fmed3f(a, b, inf); };
             lm[t] = larger(larger(larger(s[t][0][0], s[t][0][1]), larger(s[t][0][2], s[t][0][3])),
                            larger(larger(s[t][1][0], s[t][1][1]), larger(s[t][1][2], s[t][1][3])));
-            rise |= lm[t] > rmax[t] + kRaise;
+            any |= lm[t] > rise[t];
         }
-        if (__any(rise)) {
+        if (__any(any)) {
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 const float bm = across_rows(lm[t], OpMax());
-                if (bm > rmax[t] + kRaise) {   // rows whose maximum stays are left as they are
-                    const float alpha = __builtin_amdgcn_exp2f(rmax[t] - bm);
-                    rmax[t] = bm;
+                if (bm > rise[t]) {   // rows whose base stays are left as they are
+                    const float next = minus[t][0] - bm, up = minus[t][0] - next;   // up: by what the base rises as it is rounded
+                    const float alpha = rise[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-up);
+                    minus[t] = f32x4_t{next, next, next, next};
+                    rise[t] = kRaise;
                     rsum[t] *= alpha;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[t][e / 4][e % 4] -= up;
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt) o[t][dt] *= alpha;
                 }
             }
         }
     }
+    // The row's base, -inf where it has seen no key.
+    __device__ __forceinline__ float top(int t) const { return rise[t] == -INFINITY ? -INFINITY : -minus[t][0]; }
     // The weights of tile t's scores as matrix operands, and their sum.
     __device__ __forceinline__ void weigh(int t, Frag<T>& ph, Frag<T>& pl) {
-        const float base = rmax[t] == -INFINITY ? 0.f : rmax[t];   // a row that has seen no key yet
         float p[8], ps = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(s[t][e / 4][e % 4] - base);
+            p[e] = __builtin_amdgcn_exp2f(s[t][e / 4][e % 4]);
             ps += p[e];
         }
         rsum[t] += ps;
@@ -292,7 +301,7 @@ __device__ __forceinline__ void attend_few(WaveAttention<T, DH, 1>& w, const Att
     w.clear();
     const Sight see = late(__builtin_amdgcn_readfirstlane(L), hi);
     for (; i < hi; i += LANES) {
-        w.s[0][0] = w.s[0][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        w.s[0][0] = w.s[0][1] = w.minus[0];
 #pragma unroll
         for (int ds = 0; ds < NDS; ++ds) {
             // products that follow each other go to different sums: each waits for its sum's last one
@@ -334,7 +343,7 @@ __device__ __forceinline__ void join_few(const WaveAttention<T, DH, 1>& w, unsig
     float (*s_max)[16] = reinterpret_cast<float (*)[16]>(smem + DH * 256) + wave4 - wave, (*s_sum)[16] = s_max + 4;
     const float sum = across_rows(w.rsum[0], OpSum());
     if (g == 0) {
-        s_max[wave][c] = w.rmax[0];
+        s_max[wave][c] = w.top(0);
         s_sum[wave][c] = sum;
     }
 #pragma unroll
@@ -399,7 +408,7 @@ __device__ __forceinline__ void tile_step(WaveAttention<uint16_t, DH, 2>& w, uns
     }
     if (!use) return;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) w.s[t][0] = w.s[t][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 2; ++t) w.s[t][0] = w.s[t][1] = w.minus[t];
     // K and V fragments are read one product group ahead of their use (the scheduler would move the reads next to it)
     auto k_frags = [&](Frag<T> (&kf)[2], int ds) {
 #pragma unroll
@@ -542,7 +551,7 @@ __device__ __forceinline__ void join_tile(const WaveAttention<uint16_t, DH, 2>& 
     for (int t = 0; t < 2; ++t) {
         const float sum = across_rows(w.rsum[t], OpSum());
         if (g == 0) {
-            s_max[wave][t][c] = w.rmax[t];
+            s_max[wave][t][c] = w.top(t);
             s_sum[wave][t][c] = sum;
         }
 #pragma unroll
