@@ -33,9 +33,9 @@
 //    stays in registers; bound by the matrix cores, the softmax beside them and, where
 //    rows are few for their keys, by the loads: 16 sequences of 11 rows over 16384
 //    shared and 400 own slots of 40 heads of 128 (121 GFLOP with the remainders)
-//    155 us, 136 without the products and 135 without the loads; 8 blocks of 128
-//    rows over 4000 slots (136 GFLOP) 124 us, 1.10 PFLOP/s (a large product 1.19);
-//    two workgroups a CU, so 4 such blocks take 107 us.
+//    152-156 us, 136 without the products and 135 without the loads; 8 blocks of 128
+//    rows over 4000 slots (136 GFLOP) 120-124 us, 1.1 PFLOP/s (a large product 1.19);
+//    two workgroups a CU, so 4 such blocks take 106 us.
 // On bf16 models Q and P enter the matrix cores as value and remainder, as in
 // attention.hip: 16 bits of each, outputs within 3.5e-6 of their size of the
 // 64-bit result (float32 arithmetic 0.7e-6 to 2.3e-6); a third term would add
