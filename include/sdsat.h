@@ -175,7 +175,8 @@ int sdsat_verify_nucleus(sdsat_ctx* ctx, int32_t batch, int32_t q, const float* 
                          int32_t* d_n_accept);
 
 /* Log probabilities for ranking and reporting completions.  For each logits row
- * (b, j) of [batch*q, V] float32, with z = logits / temperature (> 0, finite, as is 1 / temperature):
+ * (b, j) of [batch*q, V] float32, with z = logits / temperature (> 0, finite, and so is
+ * log2(e) / temperature, by which logits are scaled: above 4.25e-39):
  *   d_logprob[b*q + j]  log softmax(z)[d_tokens[b*q + j]]; 0 where the token is
  *                       negative (a row without one); a token >= V gives NaN
  *                       and SDSAT_EDATA at the next synchronous call;

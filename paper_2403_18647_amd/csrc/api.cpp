@@ -821,8 +821,8 @@ int sdsat_token_logprobs(sdsat_ctx* c, int32_t batch, int32_t q, const float* d_
     int rc = check_block_args(c, batch, q);
     if (rc) return rc;
     if (!d_logits || (d_logprob && !d_tokens)) return fail(c, SDSAT_EINVAL, "NULL logits, or tokens with logprob");
-    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature))
-        return fail(c, SDSAT_EINVAL, "temperature and its inverse must be positive and finite");
+    if (!logprob_temperature_ok(temperature))
+        return fail(c, SDSAT_EINVAL, "temperature and log2(e) / temperature must be positive and finite");
     if (n_top < 0 || n_top > kMaxTop || n_top > c->D.V) return fail(c, SDSAT_EINVAL, "n_top must be 0..32 and at most V");
     if (n_top && (!d_top_ids || !d_top_logprobs)) return fail(c, SDSAT_EINVAL, "NULL top_ids or top_logprobs with n_top");
     if (!d_logprob && !d_entropy && !n_top) return SDSAT_OK;

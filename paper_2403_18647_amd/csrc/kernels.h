@@ -284,6 +284,10 @@ hipError_t launch_verify_nucleus(const float* logits, int B, int q, int V, const
 // Log probabilities of tokens (negative: none, 0 is written) under logits rows at a temperature, the rows' entropies
 // and n_top alternatives.  lp, ent: [M] or null; part: logprob_part_bytes; counter [M]: zero between launches
 constexpr int kMaxTop = 32;
+// what the kernel multiplies differences of logits by is finite
+inline bool logprob_temperature_ok(float t) {
+    return t > 0.f && t <= 3.402823466e38f && 1.0f / t * 1.44269504f <= 3.402823466e38f;
+}
 size_t logprob_part_bytes(int M, int V);
 hipError_t launch_token_logprobs(const float* logits, int M, int V, const int* tokens, float temperature, int n_top, float* lp,
                                  float* ent, int* ids, float* top_lp, void* part, int* counter, int* err, hipStream_t s);

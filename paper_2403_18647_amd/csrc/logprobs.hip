@@ -418,7 +418,7 @@ size_t logprob_part_bytes(int M, int V) { return V > kLpStep ? (size_t)std::min<
 
 hipError_t launch_token_logprobs(const float* logits, int M, int V, const int* tokens, float temperature, int n_top, float* lp,
                                  float* ent, int* ids, float* top_lp, void* part, int* counter, int* err, hipStream_t s) {
-    if (M < 1 || V < 1 || V > (1 << 30) || !(temperature > 0.f) || n_top < 0 || n_top > kMaxTop || n_top > V || (lp && !tokens) ||
+    if (M < 1 || V < 1 || V > (1 << 30) || !logprob_temperature_ok(temperature) || n_top < 0 || n_top > kMaxTop || n_top > V || (lp && !tokens) ||
         (n_top && (!ids || !top_lp)))
         return hipErrorInvalidValue;
     const int seg = logprob_segment(M, V, n_top), segs = (int)(((long)V + seg - 1) / seg);

@@ -1,0 +1,36 @@
+// Host-side checks of limits: what the launches of the cache reordering, the shared attention and the log probabilities
+// take and refuse at the ends of their ranges, and how large their grids and workspaces get.  Built by
+// tests/test_operator_limits_cpu.py with the host compiler against libsdsat.so; no device is touched (only invalid
+// argument sets are passed to a launch).
+#include <algorithm>
+#include <cstdio>
+#include <limits>
+
+#include "kernels.h"
+
+using namespace sdsat;
+
+static int failures = 0;
+#define CHECK(cond, ...)                      \
+    do {                                      \
+        if (!(cond)) {                        \
+            std::printf("FAIL: " __VA_ARGS__); \
+            std::printf("\n");                \
+            ++failures;                       \
+        }                                     \
+    } while (0)
+
+int main() {
+    int dummy[256] = {};
+    void* ptr = dummy;
+    float* fp = reinterpret_cast<float*>(ptr);
+    // log probabilities: temperatures by which the logits cannot be scaled
+    const float inf = std::numeric_limits<float>::infinity();
+    for (float t : {0.f, -0.f, -1.f, 1e-45f, 1e-39f, 3.0e-39f, 3.5e-39f, 4.2e-39f, inf, -inf, std::numeric_limits<float>::quiet_NaN()})
+        CHECK(launch_token_logprobs(fp, 1, 100, dummy, t, 2, fp, fp, dummy, fp, ptr, dummy, dummy, nullptr) == hipErrorInvalidValue,
+              "log probabilities accepted the temperature %g", t);
+    for (float t : {4.25e-39f, 5.877471754e-39f, 1e-30f, 1.f, 3.402823466e38f})
+        CHECK(logprob_temperature_ok(t), "the temperature %g is refused", t);
+    std::printf("ok (%d failed)\n", failures);
+    return failures != 0;
+}
