@@ -337,8 +337,8 @@ int fits(sdsat_ctx* c, int B, int q, bool* ok) {
     return SDSAT_OK;
 }
 
-// Groups of sequences that share a prefix: whole 32-slot pages of it, by group.
-struct Share { int group; int pages[kMaxShareGroups]; };
+// Groups of sequences that share a prefix: whole 32-slot pages of it and the slots left, by group.
+struct Share { int group; int pages[kMaxShareGroups], rest[kMaxShareGroups]; };
 
 // out: float rows (out_f32), or elements in fragment order of out_rows rows (B*q, or that rounded up to 16)
 int attention_layer(sdsat_ctx* c, int layer, int B, int q, const uint64_t* mask, const float* qbuf, void* out,
@@ -355,6 +355,7 @@ int attention_layer(sdsat_ctx* c, int layer, int B, int q, const uint64_t* mask,
         a.at.out = out; a.at.out_f32 = out_f32; a.at.ldo = ldo; a.at.out_rows = out_rows; a.at.err = c->err_flag;
         a.group = share->group; a.part = c->shared_part;
         std::copy(share->pages, share->pages + B / share->group, a.pages);
+        std::copy(share->rest, share->rest + B / share->group, a.rest);
         hipEvent_t e0, e1;
         prof_pair(c, PK_ATTN, &e0, &e1);
         HIPCHK(c, launch_attention_shared(D.dtype, D.Dh, p, a, c->stream, e0, e1));
@@ -565,6 +566,7 @@ int check_share(sdsat_ctx* c, int B, int group, const int32_t* h_prefix_len, Sha
             if (h_prefix_len[g] > c->len_hint[b])
                 return fail(c, SDSAT_ECAPACITY, "shared prefix longer than a sequence's committed slots");
         share->pages[g] = h_prefix_len[g] / 32;
+        share->rest[g] = h_prefix_len[g] % 32;
     }
     return SDSAT_OK;
 }

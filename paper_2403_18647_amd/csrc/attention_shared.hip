@@ -612,7 +612,7 @@ __device__ __forceinline__ void store_part(const SharedArgs& a, int row, int h, 
 }
 
 // The rows of a block of sequence b that a workgroup has, of head h.
-struct OwnRows { int h, b, m0, row0, rows, pages; };
+struct OwnRows { int h, b, m0, row0, rows, pages, prefix; };
 __device__ __forceinline__ OwnRows own_rows(const SharedArgs& a, int i, int tile, int tile_rows) {
     OwnRows o;
     o.h = i % a.at.H;
@@ -621,6 +621,7 @@ __device__ __forceinline__ OwnRows own_rows(const SharedArgs& a, int i, int tile
     o.row0 = o.b * a.at.q + o.m0;
     o.rows = min(tile_rows, a.at.q - o.m0);
     o.pages = a.pages[o.b / a.group];
+    o.prefix = 32 * o.pages + a.rest[o.b / a.group];
     return o;
 }
 // Key blocks of sequence b (rows up to m of its block): none where the cache is too short (the host checks capacity;
@@ -628,9 +629,9 @@ __device__ __forceinline__ OwnRows own_rows(const SharedArgs& a, int i, int tile
 __device__ __forceinline__ int key_blocks(const SharedArgs& a, int L, int m) {
     return L < 0 || L + a.at.q > a.at.S_max ? 0 : (L + min(m, a.at.q) + 31) / 32;
 }
-__device__ __forceinline__ void report(const SharedArgs& a, int L, int pages) {
+__device__ __forceinline__ void report(const SharedArgs& a, int L, int prefix) {
     const bool over = L < 0 || L + a.at.q > a.at.S_max;
-    if (threadIdx.x == 0 && (over || L < 32 * pages)) atomicOr(a.at.err, over ? 4 : 16);
+    if (threadIdx.x == 0 && (over || L < prefix)) atomicOr(a.at.err, over ? 4 : 16);
 }
 __device__ __forceinline__ Sight own_sight(const SharedArgs& a, int b, int L) {
     return {L, L + a.at.q, a.at.q, a.at.mask ? a.at.mask + (size_t)b * a.at.q : nullptr};
@@ -673,7 +674,7 @@ __global__ void __launch_bounds__(256, STAGED || sizeof(T) * DH > 256 ? 2 : 3) s
     WaveAttention<T, DH, 1> w;
     attend_few<T, DH, kOwnLanes>(w, a.at, head_cache<T, DH>(a.at, o.b, o.b, o.h, 0), lo, end, o.row0, o.rows, o.h, o.m0, wave,
                                  lane, a.at.cache_len + o.b, [&](int L, int& hi) {
-        if (part == 0) report(a, L, o.pages);
+        if (part == 0) report(a, L, o.prefix);
         hi = min(hi, key_blocks(a, L, a.at.q));
         return own_sight(a, o.b, L);
     });
@@ -734,7 +735,7 @@ __global__ void __launch_bounds__(256, 2) shared_rows_kernel(SharedArgs a) {
     const int tile = last && 2 * last <= TILE ? (nth + 1 == a.tiles ? nth : a.tiles - 2 - nth) : a.tiles - 1 - nth;
     const OwnRows o = own_rows(a, (int)blockIdx.x % (a.at.B * a.at.H), tile, TILE);
     const int L = __builtin_amdgcn_readfirstlane(a.at.cache_len[o.b]), nblk = key_blocks(a, L, o.m0 + TILE);   // what the tile's last row can see
-    report(a, L, o.pages);
+    report(a, L, o.prefix);
     const Sight see = own_sight(a, o.b, L);
     const HeadCache<T> hc = head_cache<T, DH>(a.at, o.b / a.group * a.group, o.b, o.h, o.pages);
     auto write = [&](int r, int d, f32x4_t acc, float, float den) {
@@ -779,7 +780,8 @@ hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p,
         (dtype != 1 && p.staged) || (dtype == 1 && p.whole && !p.staged))
         return hipErrorInvalidValue;
     for (int g = 0; g < at.B / a.group; ++g)
-        if (a.pages[g] < 0 || a.pages[g] > at.S_max / 32 || (!p.whole && a.pages[g] > p.chunk * p.prefix_parts))
+        if (a.pages[g] < 0 || a.pages[g] > at.S_max / 32 || a.rest[g] < 0 || a.rest[g] > 31 ||
+            (!p.whole && a.pages[g] > p.chunk * p.prefix_parts))
             return hipErrorInvalidValue;
     a.chunk = p.chunk; a.prefix_parts = p.prefix_parts; a.own_chunk = p.own_chunk; a.own_parts = p.own_parts;
     a.slots = p.slots; a.tiles = p.tiles; a.prefix_grid = p.prefix_grid;

@@ -156,6 +156,7 @@ struct SharedArgs {
     AttnArgs at;
     int group;
     int pages[kMaxShareGroups];
+    int rest[kMaxShareGroups];         // slots of the prefix behind its shared pages, in each sequence's own
     float* part;                       // [B*q][H][slots][Dh + 4]: O to the part's maximum, the maximum, the sum
     int chunk, prefix_parts, own_chunk, own_parts, slots, tiles, prefix_grid;
 };

@@ -24,6 +24,18 @@ int main() {
     int dummy[256] = {};
     void* ptr = dummy;
     float* fp = reinterpret_cast<float*>(ptr);
+    // shared attention: what is left of a prefix behind its pages is less than a page
+    {
+        int pages[2] = {4, 3};
+        const SharedPlan p = plan_shared(4, 2, 2, 6, 1, pages, 140, 256);
+        for (int rest : {-1, 32, 1 << 20}) {
+            SharedArgs a{};
+            a.at.qbuf = fp; a.at.kc = a.at.vc = ptr; a.at.cache_len = dummy; a.at.B = 4; a.at.q = 6; a.at.H = 2; a.at.S_max = 256;
+            a.at.out = ptr; a.at.out_f32 = 1; a.at.ldo = 128; a.at.out_rows = 24; a.at.err = dummy;
+            a.group = 2; a.pages[0] = 4; a.pages[1] = 3; a.rest[1] = rest; a.part = fp;
+            CHECK(launch_attention_shared(1, 64, p, a, nullptr) == hipErrorInvalidValue, "shared attention accepted %d slots left", rest);
+        }
+    }
     // log probabilities: temperatures by which the logits cannot be scaled
     const float inf = std::numeric_limits<float>::infinity();
     for (float t : {0.f, -0.f, -1.f, 1e-45f, 1e-39f, 3.0e-39f, 3.5e-39f, 4.2e-39f, inf, -inf, std::numeric_limits<float>::quiet_NaN()})
