@@ -562,12 +562,22 @@ int check_share(sdsat_ctx* c, int B, int group, const int32_t* h_prefix_len, Sha
     share->group = group;
     for (int g = 0; g < B / group; ++g) {
         if (h_prefix_len[g] < 0) return fail(c, SDSAT_EINVAL, "negative prefix length");
-        for (int b = g * group; b < (g + 1) * group; ++b)   // len_hint: an upper bound of the committed length
-            if (h_prefix_len[g] > c->len_hint[b])
-                return fail(c, SDSAT_ECAPACITY, "shared prefix longer than a sequence's committed slots");
         share->pages[g] = h_prefix_len[g] / 32;
         share->rest[g] = h_prefix_len[g] % 32;
     }
+    return SDSAT_OK;
+}
+
+// Whether a block of q rows fits and the prefixes are not longer than their sequences, as far as the host knows the
+// lengths: exactly where fits() has read them, else as upper bounds.
+int check_share_lens(sdsat_ctx* c, int B, int q, const Share& share) {
+    bool ok = false;
+    const int rc = fits(c, B, q, &ok);
+    if (rc) return rc;
+    if (!ok) return fail(c, SDSAT_ECAPACITY, "cache_len + q exceeds max_ctx");
+    for (int b = 0; b < B; ++b)
+        if (32 * share.pages[b / share.group] + share.rest[b / share.group] > c->len_hint[b])
+            return fail(c, SDSAT_ECAPACITY, "shared prefix longer than a sequence's committed slots");
     return SDSAT_OK;
 }
 
@@ -781,10 +791,8 @@ int sdsat_forward_block_shared(sdsat_ctx* c, int32_t batch, int32_t q, int32_t g
     Share share;
     rc = check_share(c, batch, group, h_prefix_len, &share);
     if (rc) return rc;
-    bool ok = false;
-    rc = fits(c, batch, q, &ok);
+    rc = check_share_lens(c, batch, q, share);
     if (rc) return rc;
-    if (!ok) return fail(c, SDSAT_ECAPACITY, "cache_len + q exceeds max_ctx");
     return forward_block_impl(c, batch, q, d_tokens, d_ancestor_mask, d_logits, &share);
 }
 
@@ -1134,11 +1142,9 @@ int sdsat_attention_shared(sdsat_ctx* c, int32_t layer, int32_t batch, int32_t q
     Share share;
     rc = check_share(c, batch, group, h_prefix_len, &share);
     if (rc) return rc;
-    if (group == 1) return sdsat_attention(c, layer, batch, q, d_q, d_ancestor_mask, d_out);
-    bool ok = false;
-    rc = fits(c, batch, q, &ok);
+    rc = check_share_lens(c, batch, q, share);
     if (rc) return rc;
-    if (!ok) return fail(c, SDSAT_ECAPACITY, "cache_len + q exceeds max_ctx");
+    if (group == 1) return sdsat_attention(c, layer, batch, q, d_q, d_ancestor_mask, d_out);
     return attention_layer(c, layer, batch, q, d_ancestor_mask, d_q, d_out, 1, D.d, batch * q, &share);
 }
 

@@ -31,3 +31,22 @@ def test_prefixes_longer_than_a_sequence_by_less_than_a_page(prefix, length, cod
     assert device_error(ctx) == code
     assert device_error(ctx) == 0
     ctx.close()
+
+
+@pytest.mark.parametrize("group", [1, 2])
+def test_lengths_that_the_capacity_check_reads_hold_for_the_prefix_too(group):
+    """The bounds (90) say that a block may not fit: the true lengths (30) are read, and the prefix is compared with them."""
+    ctx = grown(96, 9, 2, [30, 30], 10)
+    x = torch.zeros((18, 128), device="cuda")
+    with pytest.raises(B.SdsatError) as e:
+        B.sdsat_attention_shared(ctx.handle, 0, 2, 9, group, [31] * (2 // group), x, None, x.clone())
+    assert e.value.code == -4
+    t = torch.zeros((2, 9), dtype=torch.int32, device="cuda")
+    ctx2 = grown(96, 9, 2, [30, 30], 10)
+    with pytest.raises(B.SdsatError) as e:
+        B.sdsat_forward_block_shared(ctx2.handle, 2, 9, group, [31] * (2 // group), t, None, None)
+    assert e.value.code == -4
+    for c in (ctx, ctx2):
+        B.sdsat_attention_shared(c.handle, 0, 2, 9, group, [30] * (2 // group), x, None, x.clone())
+        assert device_error(c) == 0
+        c.close()
