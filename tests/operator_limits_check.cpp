@@ -36,6 +36,16 @@ int main() {
             CHECK(launch_attention_shared(1, 64, p, a, nullptr) == hipErrorInvalidValue, "shared attention accepted %d slots left", rest);
         }
     }
+    // the shapes of tests/test_gpu_attention_shared_parts.py cut own slots into several parts
+    {
+        struct Shape { int B, group, H, S, pages0, pages1, len, parts; };
+        for (const Shape& s : {Shape{4, 2, 2, 2752, 2, 15, 2580, 3}, Shape{4, 2, 3, 2752, 2, 15, 2580, 3}, Shape{2, 2, 32, 3424, 10, 0, 3333, 3},
+                               Shape{4, 4, 32, 3424, 10, 0, 3333, 3}, Shape{3, 3, 32, 3424, 10, 0, 3333, 3}, Shape{2, 2, 2, 2336, 2, 0, 2112, 3}}) {
+            const int pages[2] = {s.pages0, s.pages1};
+            const SharedPlan p = plan_shared(s.B, s.group, s.H, 1, 1, pages, s.len, s.S);
+            CHECK(p.own_parts >= s.parts, "%d sequences of %d heads: %d own parts", s.B, s.H, p.own_parts);
+        }
+    }
     // log probabilities: temperatures by which the logits cannot be scaled
     const float inf = std::numeric_limits<float>::infinity();
     for (float t : {0.f, -0.f, -1.f, 1e-45f, 1e-39f, 3.0e-39f, 3.5e-39f, 4.2e-39f, inf, -inf, std::numeric_limits<float>::quiet_NaN()})
