@@ -180,6 +180,7 @@ hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p,
 // line each), and 6 * all
 constexpr int kReorderMaxBatch = 1024, kReorderCounts = 16, kReorderHead = 32 * (1 + kReorderCounts) + 32;
 bool reorder_supported(int esz, int all, int n_layers, int H, int Dh, int S_max);
+long reorder_workgroups(int esz, int n_layers, int H, int Dh, int max_len, int first_slot);
 hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n_layers, int batch, int all, int H, int Dh,
                           int S_max, int* cache_len, int max_len, const int* src, int first_slot, int* steps, int* err,
                           hipStream_t s);

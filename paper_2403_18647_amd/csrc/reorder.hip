@@ -169,7 +169,8 @@ struct ReorderArgs {
 };
 
 // Chunks of 256 * kReorderCells cells of the pages from `first` on, of each layer, K and V, and head.  The host's grid holds
-// them all as far as it knows the lengths; workgroups take further ones where the device's are longer (a replayed graph).
+// them all as far as it knows the lengths and a launch may; workgroups take further ones where the device's lengths are
+// longer (a replayed graph), or there are more.
 static constexpr int kReorderCells = 2, kReorderAlone = 8192;   // cells per thread; workgroups that make the list themselves, at most
 template <bool AHEAD>
 __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderArgs a) {
@@ -260,10 +261,19 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderArgs a) {
     }
 }
 
-// Sequences that one workgroup's threads hold, slots that a float holds, chunks that a grid holds.
+// Sequences that one workgroup's threads hold, slots that a float holds, chunks that their 32-bit number holds.
 bool reorder_supported(int esz, int all, int n_layers, int H, int Dh, int S_max) {
     const long cells = (long)S_max * (Dh * esz / 16), most = (cells + 256 * kReorderCells - 1) / (256 * kReorderCells) * 2 * H * n_layers;
     return all <= kReorderMaxBatch && S_max < 1 << 24 && most <= 0x7FFFFFFF;
+}
+
+// One workgroup per chunk as far as the host knows the lengths; a launch holds fewer than 2^32 threads, so of larger caches
+// (7B heads and layers: from 262144 slots on) each workgroup takes several.
+long reorder_workgroups(int esz, int n_layers, int H, int Dh, int max_len, int first_slot) {
+    const int first = first_slot / 32 * 32, end = (max_len + 31) / 32 * 32;
+    const size_t cells = (size_t)std::max(0, end - first) * (Dh * esz / 16);
+    const long chunks = (long)((cells + 256 * kReorderCells - 1) / (256 * kReorderCells));
+    return std::min<long>(std::max<long>(1, chunks * 2 * H * n_layers), 0xFFFFFFFFu / 256);
 }
 
 hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n_layers, int batch, int all, int H, int Dh,
@@ -272,12 +282,10 @@ hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n
     if (batch < 1 || batch > all || all > kReorderMaxBatch || (Dh * esz) % 16 || first_slot < 0 || S_max % 32 ||
         max_len < 0 || max_len > S_max || !src || !steps)
         return hipErrorInvalidValue;
-    const int first = first_slot / 32 * 32, end = (max_len + 31) / 32 * 32;
-    const int slot_cells = Dh * esz / 16;
-    const size_t cells = (size_t)std::max(0, end - first) * slot_cells;
-    const long chunks = (long)((cells + 256 * kReorderCells - 1) / (256 * kReorderCells)), items = chunks * 2 * H * n_layers;
     if (!reorder_supported(esz, all, n_layers, H, Dh, S_max)) return hipErrorInvalidValue;
-    const bool ahead = all > 64 || items > kReorderAlone;
+    const int slot_cells = Dh * esz / 16;
+    const long groups = reorder_workgroups(esz, n_layers, H, Dh, max_len, first_slot);
+    const bool ahead = all > 64 || groups > kReorderAlone;
     if (ahead) {
         hipLaunchKernelGGL(reorder_plan_kernel, dim3(1), dim3((all + 63) / 64 * 64), 0, s, cache_len, batch, all, S_max, src,
                            reinterpret_cast<int2*>(steps + kReorderHead), steps + kReorderHead - 2, err);
@@ -287,11 +295,12 @@ hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n
     ReorderArgs a{};
     a.kc = static_cast<u32x4_t*>(kc); a.vc = static_cast<u32x4_t*>(vc);
     a.layer_cells = layer_elems * esz / 16; a.head_cells = (size_t)S_max * slot_cells;
-    a.n_layers = n_layers; a.batch = batch; a.all = all; a.H = H; a.S_max = S_max; a.slot_cells = slot_cells; a.first = first;
+    a.n_layers = n_layers; a.batch = batch; a.all = all; a.H = H; a.S_max = S_max; a.slot_cells = slot_cells;
+    a.first = first_slot / 32 * 32;
     a.cache_len = cache_len; a.src = src; a.steps = reinterpret_cast<const int2*>(steps + kReorderHead);
     a.n_steps = steps + kReorderHead - 2;
     a.arrived = steps; a.err = err;
-    const dim3 grid((unsigned)std::max<long>(1, items));
+    const dim3 grid((unsigned)groups);
     if (ahead) hipLaunchKernelGGL(reorder_copy_kernel<true>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(reorder_copy_kernel<false>, grid, dim3(256), 0, s, a);
     return hipGetLastError();

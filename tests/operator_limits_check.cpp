@@ -24,6 +24,22 @@ int main() {
     int dummy[256] = {};
     void* ptr = dummy;
     float* fp = reinterpret_cast<float*>(ptr);
+    // reordering: a launch holds fewer than 2^32 threads of 256-thread workgroups, one per 8 KiB of a moved row until then
+    {
+        struct Cache { int esz, L, H, Dh, S; };
+        for (const Cache& c : {Cache{2, 32, 32, 128, 262112}, Cache{2, 32, 32, 128, 262144}, Cache{2, 32, 32, 128, 1 << 20},
+                               Cache{4, 40, 40, 128, 1 << 19}, Cache{2, 1, 1, 64, (1 << 24) - 32}, Cache{2, 128, 127, 64, 1 << 21}}) {
+            CHECK(reorder_supported(c.esz, 4, c.L, c.H, c.Dh, c.S), "a cache of %d slots is refused", c.S);
+            for (int len : {c.S, c.S - 31, 1, 0})
+                for (int first : {0, 32, 4096, c.S}) {
+                    const size_t row = (size_t)std::max(0, (len + 31) / 32 * 32 - first / 32 * 32) * c.Dh * c.esz;
+                    const size_t chunks = (row + 8191) / 8192 * 2 * c.H * c.L;
+                    const long n = reorder_workgroups(c.esz, c.L, c.H, c.Dh, len, first);
+                    CHECK(n >= 1 && (unsigned long)n * 256 < 1ul << 32, "%ld workgroups", n);
+                    CHECK((size_t)n == std::max<size_t>(1, chunks) || chunks * 256 >= 1ul << 32, "%ld workgroups for %zu chunks", n, chunks);
+                }
+        }
+    }
     // shared attention: what is left of a prefix behind its pages is less than a page
     {
         int pages[2] = {4, 3};
