@@ -208,8 +208,6 @@ void carve(sdsat_ctx* c, Carver& cv) {
     const size_t m16 = align_up((size_t)D.maxM, 16);   // large blocks keep whole 16-row tiles
     c->obuf = cv.take(m16 * D.d_pad * e);
     c->ubuf = cv.take(m16 * D.F_pad * e);
-    c->attn_part_floats = std::max<size_t>(1, attention_partial_floats(D.maxB, D.H, D.maxQ, D.Dh, D.S));
-    c->attn_part = (float*)cv.take(c->attn_part_floats * 4);
     c->attn_ctr = (int*)cv.take(attention_counter_ints(D.maxB, D.H, D.maxQ) * 4);
     {
         const int rows = std::min(D.maxM, kSkinnyRows);
@@ -217,8 +215,6 @@ void carve(sdsat_ctx* c, Carver& cv) {
                                      gemm_resid_part_bytes(D.nt_down, D.ks_f, rows));
         c->gemm_part = part ? (float*)cv.take(part) : nullptr;
     }
-    c->shared_part_floats = shared_partial_floats_most(D.maxB, D.H, D.maxQ, D.Dh);
-    c->shared_part = (float*)cv.take(c->shared_part_floats * 4);
     c->reorder_steps = (int*)cv.take((kReorderHead + 6 * (size_t)D.maxB) * 4);
     c->lp_part = cv.take(logprob_part_bytes(D.maxM, D.V));
     c->lp_ctr = (int*)cv.take((size_t)D.maxM * 4);
@@ -244,9 +240,18 @@ void carve(sdsat_ctx* c, Carver& cv) {
     c->tree_target = (int*)cv.take(bq * 4);
     c->tree_rows = (int*)cv.take(bq * 4);
     c->tree_mask = (uint64_t*)cv.take(bq * 8);
-    c->logits = (float*)cv.take(bq * D.V * 4);
     c->hbuf = cv.take(m16 * D.d_pad * e);
-    if (D.maxM > kSkinnyRows) c->c_y = (float*)cv.take((size_t)D.maxM * D.d * 4 * kPrefillMaxSplit);   // split-K parts
+    // Neighbours, over which the parts of shared-prefix attention lie: the other attention's parts, the generation loop's
+    // logits (the loop makes no shared attention) and the split-K parts of large blocks' residual GEMMs (none are pending
+    // while an attention runs).
+    const size_t scratch = align_up(cv.off, 256);
+    c->attn_part_floats = std::max<size_t>(1, attention_partial_floats(D.maxB, D.H, D.maxQ, D.Dh, D.S));
+    c->attn_part = (float*)cv.take(c->attn_part_floats * 4);
+    c->logits = (float*)cv.take(bq * D.V * 4);
+    if (D.maxM > kSkinnyRows) c->c_y = (float*)cv.take((size_t)D.maxM * D.d * 4 * kPrefillMaxSplit);
+    c->shared_part_floats = shared_partial_floats_most(D.maxB, D.H, D.maxQ, D.Dh, D.S);
+    c->shared_part = c->attn_part;
+    cv.off = std::max(cv.off, scratch + c->shared_part_floats * 4);
 }
 
 void* layer_k(sdsat_ctx* c, int l) { return (char*)c->kc + (size_t)l * c->layer_elems * c->D.esz; }

@@ -69,6 +69,10 @@ static constexpr int kTileRows = 64;                    // rows of a workgroup t
 // 39.9), so large groups are cut for speculative blocks.
 static int shared_parts(int group) { return group < kSharedMany ? kSharedParts : kSharedManyParts; }
 
+static constexpr int kOwnPages = 32;   // pages of an own part at the least: 1024 slots
+static int prefix_parts_most(int G, int group, int H) { return std::min(kSharedMaxParts, std::max(1, shared_parts(group) / (G * H))); }
+static int own_parts_most(int B, int group, int H) { return std::min(kSharedMaxOwn, std::max(1, shared_parts(group) / (B * H))); }
+
 SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pages, int max_len, int S_max) {
     SharedPlan p{};
     const int G = B / group;
@@ -87,13 +91,13 @@ SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pag
         return p;
     }
     // pages per prefix part: four for each lane at the least
-    const int parts = std::min(kSharedMaxParts, std::max(1, shared_parts(group) / (G * H)));
+    const int parts = prefix_parts_most(G, group, H);
     p.chunk = std::max(4 * kPrefixLanes, (most + parts - 1) / parts);
     p.prefix_parts = (most + p.chunk - 1) / p.chunk;
-    // pages per own part: the own slots of a full cache in as many parts as that allows, 1024 slots at the least
+    // pages per own part: the own slots of a full cache in as many parts as that allows
     const int cap = S_max / 32 - least;
-    const int own = std::min(kSharedMaxOwn, std::max(1, shared_parts(group) / (B * H)));
-    p.own_chunk = std::max(32, (cap + own - 1) / own);
+    const int own = own_parts_most(B, group, H);
+    p.own_chunk = std::max(kOwnPages, (cap + own - 1) / own);
     const int nblk = std::max(1, std::min(cap, (max_len + q + 31) / 32 - least));
     p.own_parts = (nblk + p.own_chunk - 1) / p.own_chunk;
     p.slots = p.prefix_parts + p.own_parts;
@@ -108,15 +112,17 @@ size_t shared_partial_floats(const SharedPlan& p, int B, int q, int H, int head_
     return (size_t)B * q * H * p.slots * (head_dim + 4);
 }
 
-// The most any call can need: every row of a decode block, both kinds of part at their most.
-size_t shared_partial_floats_most(int B_max, int H, int q_max, int head_dim) {
-    if (B_max < 2) return 0;   // a group of one takes the plain attention
-    const int parts = std::min(kSharedMaxParts, std::max(1, kSharedParts / H));
+// The most any call can need: every row of a decode block, for any groups (of two sequences or more: one takes the plain
+// attention), both kinds of part at their most for a cache of S_max slots.
+size_t shared_partial_floats_most(int B_max, int H, int q_max, int head_dim, int S_max) {
+    const int pages = S_max / 32;
     size_t most = 0;
-    for (int B = 2; B <= B_max; ++B) {
-        const int own = std::min(kSharedMaxOwn, std::max(1, kSharedParts / (B * H)));
-        most = std::max(most, (size_t)B * std::min(q_max, kAttnSplitRows) * H * (parts + own) * (head_dim + 4));
-    }
+    for (int G = 1; G <= kMaxShareGroups; ++G)
+        for (int group = 2; (long)G * group <= B_max; ++group) {
+            const int B = G * group, parts = std::min(prefix_parts_most(G, group, H), pages / (4 * kPrefixLanes) + 1),
+                      own = std::min(own_parts_most(B, group, H), pages / kOwnPages + 1);
+            most = std::max(most, (size_t)B * std::min(q_max, kAttnSplitRows) * H * (parts + own) * (head_dim + 4));
+        }
     return most;
 }
 

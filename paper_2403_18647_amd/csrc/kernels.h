@@ -170,7 +170,7 @@ struct SharedPlan {
 inline bool shared_supported(int S_max, int head_dim, int esz) { return (size_t)S_max * head_dim * esz <= 0xFFF00000u; }
 SharedPlan plan_shared(int B, int group, int H, int q, int dtype, const int* pages, int max_len, int S_max);
 size_t shared_partial_floats(const SharedPlan& p, int B, int q, int H, int head_dim);
-size_t shared_partial_floats_most(int B_max, int H, int q_max, int head_dim);
+size_t shared_partial_floats_most(int B_max, int H, int q_max, int head_dim, int S_max = 0x7FFFFFFF);
 hipError_t launch_attention_shared(int dtype, int head_dim, const SharedPlan& p, SharedArgs a, hipStream_t s,
                                    hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);
 

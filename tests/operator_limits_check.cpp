@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cstdio>
 #include <limits>
+#include <vector>
 
 #include "kernels.h"
 
@@ -61,6 +62,31 @@ int main() {
             const SharedPlan p = plan_shared(s.B, s.group, s.H, 1, 1, pages, s.len, s.S);
             CHECK(p.own_parts >= s.parts, "%d sequences of %d heads: %d own parts", s.B, s.H, p.own_parts);
         }
+    }
+    // the parts of every plan fit what a context of these sizes reserves
+    {
+        struct Cfg { int maxB, H, Dh, maxQ, S; };
+        for (const Cfg& c : {Cfg{4, 4, 64, 6, 128}, Cfg{64, 4, 64, 64, 128}, Cfg{8, 32, 128, 64, 1312}, Cfg{16, 40, 128, 1024, 16896},
+                             Cfg{64, 2, 128, 11, 4096}, Cfg{24, 8, 64, 300, 608}, Cfg{2, 1, 64, 1, 32}, Cfg{130, 3, 64, 2, 96}, Cfg{64, 32, 128, 64, 4096}}) {
+            const size_t have = shared_partial_floats_most(c.maxB, c.H, c.maxQ, c.Dh, c.S);
+            for (int B = 2; B <= c.maxB; ++B)
+                for (int group = 2; group <= B; ++group) {
+                    if (B % group || B / group > kMaxShareGroups) continue;
+                    for (int most = 0; most < c.S / 32; most += 1 + most / 3)
+                        for (int other : {0, most / 2, most}) {   // the pages of the other groups
+                            std::vector<int> pages(B / group, other);
+                            pages[0] = most;
+                            for (int q : {1, std::min(c.maxQ, kAttnSplitRows)})
+                                for (int len : {32 * most, c.S - q}) {
+                                    if (len < 32 * most || len + q > c.S) continue;
+                                    const SharedPlan p = plan_shared(B, group, c.H, q, 1, pages.data(), len, c.S);
+                                    CHECK(shared_partial_floats(p, B, q, c.H, c.Dh) <= have, "B %d group %d q %d, %d pages: %zu of %zu",
+                                          B, group, q, most, shared_partial_floats(p, B, q, c.H, c.Dh), have);
+                                }
+                        }
+                }
+        }
+        CHECK(shared_partial_floats_most(1, 32, 64, 128, 4096) == 0, "one sequence shares nothing");
     }
     // log probabilities: temperatures by which the logits cannot be scaled
     const float inf = std::numeric_limits<float>::infinity();
