@@ -214,7 +214,11 @@ int sdsat_commit_kv(sdsat_ctx* ctx, int32_t batch, int32_t q, const int32_t* d_n
  * ones before are left as they are (a prefix that the sequences share or all
  * hold).  Slots past cache_len are unspecified afterwards (a block's tentative
  * rows do not move).  In place; needs max_batch <= 1024 and max_ctx below 2^24.
- * Stream-ordered. */
+ * Later calls are planned by upper bounds of the lengths that the host keeps: as
+ * only the device knows the sources, those of the batch become the largest of all
+ * max_batch sequences.  sdsat_reset of sequences out of use keeps them low, and
+ * sdsat_set_cache_len makes them exact (a block that does not fit by them reads
+ * the lengths, which a captured call cannot).  Stream-ordered. */
 int sdsat_kv_reorder(sdsat_ctx* ctx, int32_t batch, const int32_t* d_src, int32_t first_slot);
 
 /* Device pointers to one layer of the cache in the configuration's type, for

@@ -33,9 +33,11 @@
 //    stays in registers; bound by the matrix cores, the softmax beside them and, where
 //    rows are few for their keys, by the loads: 16 sequences of 11 rows over 16384
 //    shared and 400 own slots of 40 heads of 128 (121 GFLOP with the remainders)
-//    152-156 us, 136 without the products and 135 without the loads; 8 blocks of 128
-//    rows over 4000 slots (136 GFLOP) 120-124 us, 1.1 PFLOP/s (a large product 1.19);
-//    two workgroups a CU, so 4 such blocks take 106 us.
+//    150-152 us, 130 without products and softmax and 120 without the loads; 8 blocks
+//    of 128 rows over 4000 slots (136 GFLOP) 120 us, 1.1 PFLOP/s (a large product
+//    1.19); two workgroups a CU, so 4 such blocks take 90 us.
+// Float models take the first kind for every block: 4 blocks of 150 rows over 2000
+// slots 35 us with 4 heads of 64, 302 with 32 heads of 128 (20 GFLOP, 68 TFLOP/s).
 // On bf16 models Q and P enter the matrix cores as value and remainder, as in
 // attention.hip: 16 bits of each, outputs within 3.5e-6 of their size of the
 // 64-bit result (float32 arithmetic 0.7e-6 to 2.3e-6); a third term would add
@@ -63,10 +65,10 @@ static constexpr int kPrefixLanes = 2, kOwnLanes = 4;   // key lanes
 static constexpr int kTileRows = 64;                    // rows of a workgroup that stages K and V in LDS
 
 // Parts of all groups and heads.  More of them bring more waves where rows are few, fewer of them fewer partial results
-// where there are many: of one group over 6000 shared slots, 32 heads of 128, us per call with 256, 384 and 512 parts:
-// 2 sequences of 6 rows 32.4, 26.8, 31.3; 4 of 1 row 33.7, 30.8, 31.6; 12 of 6 rows 47.6, 54.1, 55.4; over 4000 slots, 16
-// of 6 rows 42.9, 50.0, 52.0; 32 of 6 rows 73.2, 78.3, 86.4.  The rows of a block have no say (16 of 1 row: 46.4, 39.0,
-// 39.9), so large groups are cut for speculative blocks.
+// where there are many: of one group over 6000 shared and 100 own slots, 32 heads of 128, us per call with 256, 384 and 512
+// parts: 2 sequences of 6 rows 24.6, 22.3, 26.0; 4 of 1 row 25.0, 24.4, 25.8; 12 of 6 rows 41.7, 42.7, 49.9; over 4000
+// slots, 16 of 6 rows 36.3, 40.9, 45.1; 32 of 6 rows 57.1, 65.8, 74.5.  The rows of a block have no say (16 of 1 row: 27.2,
+// 24.9, 25.4), so large groups are cut for speculative blocks.
 static int shared_parts(int group) { return group < kSharedMany ? kSharedParts : kSharedManyParts; }
 
 static constexpr int kOwnPages = 32;   // pages of an own part at the least: 1024 slots

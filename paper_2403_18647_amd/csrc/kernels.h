@@ -147,8 +147,8 @@ constexpr int kSharedParts = 384;      // parts the shared pages of all groups a
 constexpr int kSharedManyParts = 256;  // the same for groups of kSharedMany sequences or more
 constexpr int kSharedMany = 16;
 // Groups of more rows stage K and V in LDS (bf16).  4000 shared slots, 32 heads of 128, us from registers and from LDS:
-// 8 sequences of 1 row 21.5, 22.5; 2 of 6 rows 18.5, 21.9; 4 of 4 rows 21.0, 22.6; 4 of 6 rows 26.0, 23.5; 8 of 4 rows
-// 30.4, 24.6; 8 of 6 rows 38.4, 26.9
+// 8 sequences of 1 row 20.9, 21.8; 2 of 6 rows 18.1, 21.3; 4 of 4 rows 20.7, 21.9; 4 of 6 rows 25.3, 22.8; 8 of 4 rows
+// 29.3, 23.6; 8 of 6 rows 37.6, 25.6
 constexpr int kSharedFewRows = 16;
 constexpr int kSharedMaxParts = 32;    // parts of a prefix, at most
 constexpr int kSharedMaxOwn = 8;       // parts of a sequence's own slots, at most

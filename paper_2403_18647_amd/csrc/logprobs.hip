@@ -23,6 +23,13 @@
 // candidates than LDS holds (many equal values) take their ids one after the
 // other.  The segment that arrives last joins the row's results in segment order.
 //
+// The threshold has the 16 leading bits of a logit, steps of 2^-7 of its size: rows
+// whose logits lie close together for their size, or are equal in many ids, have
+// more candidates than LDS holds and pay for it (us with 1, 5 and 20 alternatives;
+// ordinary rows of N(0, 4) take 47, 49 and 63, every row 42 without any): 2047 rows
+// of 32016 ids of 20 + N(0, 0.01) 176, 428, 1421; of 1000 + N(0, 4) 57, 71, 408; all
+// equal 174, 401, 1226.
+//
 // Bound by HBM over many rows: 2047 rows of 32016 ids with one alternative take
 // 50 us, 5.2 TB/s (a large copy here reaches 4.9, a read 6.3).  Over few rows the
 // way from the last load to the result counts: 96 rows of 128256 ids take 17.7 us
@@ -44,7 +51,8 @@ static constexpr int kLpTile = 64 * 4 * kLpVec;               // ids a wave take
 static constexpr int kLpStep = kLpWaves * kLpTile;            // segments are multiples of it
 static constexpr int kLpFew = 384;                            // candidates of a segment that are ranked, at most
 static constexpr int kLpGrid = 1024;                          // rows are cut into as many segments together, at most: four
-                                                              // workgroups a CU; 96 rows of 128256 took 24 us, with 2048 26
+                                                              // workgroups a CU; 96 rows of 128256 take 17.7 us, with 512
+                                                              // 17.9, with 2048 20.9
 static constexpr int kLpSegments = 64, kLpKeys = 1024;        // segments of a row, and their keys in the join, at most
 static_assert(kMaxTop <= 64, "lanes for the thresholds");
 

@@ -16,13 +16,15 @@
 // themselves first); each cycle begins by holding one member's cell in a second
 // register.  For up to 64 sequences and 8192 workgroups every workgroup makes
 // the list itself, in one wave, and the last one to finish writes the new
-// lengths (one launch instead of two: four sequences of a tiny decoder 7.9 ->
-// 5.1 us, one page of eight sequences in eight 7B layers 11.9 -> 9.2; 20160
-// workgroups 455 -> 473); else one workgroup makes it in a launch ahead.
+// lengths (one launch instead of two: four sequences of a tiny decoder 8.2 ->
+// 5.3 us, one page of eight sequences in eight 7B layers 10.4 -> 9.3, 8192
+// workgroups 41.7 -> 39.0; but 20160 209.7 -> 213.8, 40000 436 -> 452); else one
+// workgroup makes it in a launch ahead.
 // Nothing is computed: each source's pages are read once, each destination's
 // written once, and the copy is bound by HBM: 16 sequences of 4000 slots
-// compacted in four 13B layers (2.47 GB) 432 us, 5.7 TB/s; nontemporal stores,
-// which nothing of this call reads again (ordinary ones 454 us).
+// compacted in four 13B layers (2.47 GB) 432-437 us, 5.7 TB/s; nontemporal stores,
+// which nothing of this call reads again (ordinary ones 456 us; eight beams of 790
+// slots in eight 7B layers 40 and 54).
 #include <algorithm>
 
 #include "device.h"
