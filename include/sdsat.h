@@ -218,7 +218,9 @@ int sdsat_commit_kv(sdsat_ctx* ctx, int32_t batch, int32_t q, const int32_t* d_n
  * only the device knows the sources, those of the batch become the largest of all
  * max_batch sequences.  sdsat_reset of sequences out of use keeps them low, and
  * sdsat_set_cache_len makes them exact (a block that does not fit by them reads
- * the lengths, which a captured call cannot).  Stream-ordered. */
+ * the lengths, which a captured call cannot).  A captured sdsat_kv_reorder or
+ * sdsat_commit_kv moves them when it is captured, not when it is replayed: call
+ * sdsat_set_cache_len where replays have made sequences longer.  Stream-ordered. */
 int sdsat_kv_reorder(sdsat_ctx* ctx, int32_t batch, const int32_t* d_src, int32_t first_slot);
 
 /* Device pointers to one layer of the cache in the configuration's type, for
