@@ -193,6 +193,32 @@ int sdsat_token_logprobs(sdsat_ctx* ctx, int32_t batch, int32_t q, const float* 
                          const int32_t* d_tokens, float temperature, int32_t n_top, float* d_logprob,
                          float* d_entropy, int32_t* d_top_ids, float* d_top_logprobs);
 
+/* What a token may not be, or is less likely to be: rules for the logits of a block's
+ * rows ahead of verification.  Any pointer may be NULL (that rule is left out). */
+typedef struct sdsat_logit_rules {
+    /* the tokens each sequence holds, committed ones: [batch, history_ld], the first
+     * d_history_len[b] (0..history_ld; SDSAT_EDATA otherwise) of a row, d_prompt_len[b]
+     * of them (NULL: none) the prompt.  Ids outside 0..V-1 count as no token. */
+    const int32_t* d_history; const int32_t* d_history_len; const int32_t* d_prompt_len;
+    int32_t history_ld;            /* below 2^24 */
+    /* the block's tokens [batch, q], as fed to sdsat_forward_block (drafts count for the
+     * rows behind them), and what each row sees of them, as sdsat_forward_block's masks
+     * (NULL: rows 0..j).  q <= 64. */
+    const int32_t* d_tokens; const uint64_t* d_mask;
+    const float* d_penalties;      /* [3, batch]: repetition (> 0), frequency, presence */
+    const float* d_bias; int64_t bias_ld;             /* [V] or, with bias_ld >= V, a row per sequence */
+    const uint32_t* d_allowed; int32_t allowed_ld;    /* [batch*q, allowed_ld]: bit v % 32 of word v / 32 */
+} sdsat_logit_rules;
+
+/* Adjust logits rows (b, j) of [batch*q, V]: with said = the times v stands in the
+ * history behind the prompt and among the block's tokens that row j sees, and seen = v
+ * stands there or in the prompt,
+ *   z = seen ? (z > 0 ? z / repetition : z * repetition) : z
+ *   z = z - frequency * said - presence * [said > 0] + bias[v], -inf where v is not allowed.
+ * d_out may be d_logits.  A row that loses every id is all -inf.  Stream-ordered. */
+int sdsat_adjust_logits(sdsat_ctx* ctx, int32_t batch, int32_t q, const float* d_logits,
+                        const sdsat_logit_rules* rules, float* d_out);
+
 /* Commit block rows to the KV cache (the step after Eq. 1 keeps row 0, the
  * step after Eq. 3 keeps rows 0..m).  d_n_commit[b] rows of sequence b become
  * committed: cache_len[b] += n.  d_rows NULL: the committed rows are block rows
@@ -277,6 +303,107 @@ int sdsat_generate_forced(sdsat_ctx* ctx, int32_t batch, const int32_t* h_prompt
                           int32_t max_new, int32_t k, const int32_t* h_adaptive_ids, int32_t mode,
                           float temperature, float top_p, int32_t top_k, uint64_t seed,
                           const int32_t* h_ref, int32_t ref_len, int32_t* h_out, sdsat_stats* h_stats);
+
+/* ---- paged cache: many sequences in one pool ----
+ *
+ * For programs that serve sequences of unequal lengths which come and go: K and V of a
+ * layer lie in a pool of 32-slot pages, a table names each sequence's pages, and one call
+ * takes chunks of any lengths together - pieces of prompts, draft and verify blocks, single
+ * tokens.  Query heads may share key heads (n_heads a multiple of n_kv_heads).
+ *
+ * A layer's pool, owned by the caller, in the configuration's type:
+ *   K [n_pages][n_kv_heads][32][head_dim], V [n_pages][n_kv_heads][head_dim][32], the slot
+ *   16a + 4g + r of a page (a < 2, g < 4, r < 4) at place 8g + 4a + r of V
+ * (whole pages move between this and sdsat_cache_ptr's layout as they are).  Contents of
+ * slots that no row sees are of no account, infinities and NaN among them. */
+#define SDSAT_PAGE 32
+
+typedef struct sdsat_paged sdsat_paged;   /* opaque, library-owned handle */
+
+typedef struct sdsat_paged_config {
+    int32_t n_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
+    int32_t dtype;                           /* of the pool, queries and (or float) outputs */
+    int32_t n_pages;                         /* pages of each pool */
+    int32_t max_rows;                        /* new tokens of a call, of all its sequences */
+    int32_t max_batch;                       /* sequences of a call */
+    int32_t max_ctx;                         /* slots of a sequence, at most 2^24 */
+} sdsat_paged_config;
+
+/* The sequences of a call.  Sequence b has rows d_start[b] .. d_start[b+1] - 1 of the call's
+ * arrays (none is allowed), the new tokens at slots d_len[b] .. of it; slot s lies in page
+ * d_pages[b * pages_ld + s / 32].  Entries of the table that no new (appending) or visible
+ * (attention) slot needs are not used.  Rows behind d_start[batch] are left as they are.
+ * The host's bounds max_q >= new tokens of each sequence and max_len >= its slots with the
+ * new tokens shape the launch; a sequence past them, or with negative or descending
+ * numbers, is left out and reported by sdsat_paged_status, as are pages outside the pool
+ * (what such a sequence would have got is unspecified). */
+typedef struct sdsat_paged_batch {
+    const int32_t* d_start;   /* [batch + 1] */
+    const int32_t* d_len;     /* [batch]: cached slots ahead of the new tokens */
+    const int32_t* d_pages;   /* [batch, pages_ld] */
+    int32_t batch, pages_ld;
+    int32_t rows;             /* rows of the call's arrays */
+    int32_t max_q, max_len;
+} sdsat_paged_batch;
+
+#define SDSAT_ROPE_HALF 0          /* pairs (j, j + rot_dims / 2) */
+#define SDSAT_ROPE_INTERLEAVED 1   /* pairs (2j, 2j + 1) */
+#define SDSAT_ROPE_PLAIN 0         /* f_j = base^(-2j / rot_dims) */
+#define SDSAT_ROPE_LINEAR 1        /* f_j / factor */
+#define SDSAT_ROPE_NTK 2           /* base * factor^(rot_dims / (rot_dims - 2)) for base */
+#define SDSAT_ROPE_PARTS 3         /* f_j where ctx holds more than `high` of its turns, f_j / factor where fewer
+                                      than `low`, between them in proportion */
+
+/* Rotary positions: the first rot_dims columns of a head are turned by position * f_j, cosines
+ * and sines multiplied by mscale.  Filled by sdsat_rope_init, or by the caller. */
+typedef struct sdsat_rope {
+    int32_t layout, rot_dims;   /* rot_dims a multiple of 8, at most head_dim; 0: no rotation */
+    float mscale;
+    double turns[64];           /* f_j / (2 pi) */
+} sdsat_rope;
+
+/* factor is read by the last three scalings, ctx, low and high by SDSAT_ROPE_PARTS.  Host-only. */
+int sdsat_rope_init(int32_t layout, int32_t rot_dims, double base, int32_t scaling, double factor,
+                    double ctx, double low, double high, float mscale, sdsat_rope* out);
+
+/* A handle for calls on one stream, for all layers (of one shape).  Workspace: device memory of
+ * sdsat_paged_query_sizes() bytes, 256-byte aligned, the caller's, for the handle's lifetime; calls
+ * on one handle, captured ones too, must not overlap.  sdsat_paged_init is synchronous. */
+int sdsat_paged_query_sizes(const sdsat_paged_config* cfg, size_t* workspace_bytes);
+int sdsat_paged_init(const sdsat_paged_config* cfg, void* workspace, size_t workspace_bytes,
+                     void* hip_stream, sdsat_paged** out);
+
+/* Append the new tokens' keys and values.  d_x: rows q | k | v ([rows, ld_x], n_heads, n_kv_heads
+ * and n_kv_heads heads of head_dim; x_dtype fp32 or bf16).  In float: heads of q and k are
+ * multiplied by gain / sqrt(mean of squares + eps) where d_q_gain or d_k_gain ([head_dim] float) is
+ * not NULL, then turned by `rope` (NULL: not) at position d_pos[row] (NULL: the slot); K and V go
+ * to the pages, q to d_q ([rows, ld_q], the pool's type).  One rounding to the type.  Two rows
+ * must not have the same slot of the same page.  Strides are in elements, multiples of 8; the
+ * arrays are 16-byte aligned and do not overlap.  Stream-ordered. */
+int sdsat_paged_append(sdsat_paged* paged, const sdsat_paged_batch* batch, void* d_k, void* d_v,
+                       const void* d_x, int32_t x_dtype, int64_t ld_x, const sdsat_rope* rope,
+                       const int32_t* d_pos, const float* d_q_gain, const float* d_k_gain, float eps,
+                       void* d_q, int64_t ld_q);
+
+/* Attention of the new tokens' queries d_q ([rows, ld_q], the pool's type) over their sequences' pages,
+ * which hold the new tokens too.  A row at slot s sees slots 0..s, with window > 0 the last `window` of
+ * them (s among them).  With d_mask ([rows] uint64, max_q <= 64, no window) it sees the slots below
+ * d_len and of its chunk's rows j those with bit j set.  A row that sees nothing gives zeros.
+ * scale 0: 1 / sqrt(head_dim).  d_out: [rows, ld_out], the pool's type or fp32.  Scores, sums and
+ * outputs are accumulated in float; the weights are rounded to the pool's type.  A row's result
+ * depends on its sequence alone, not on the rest of the call; while a chunk has at most 64 query heads
+ * per key head and token (rows * n_heads / n_kv_heads <= 64) nor on the chunk's length: a token decoded
+ * alone and the same token in a draft block give the same bits.  Stream-ordered. */
+int sdsat_paged_attention(sdsat_paged* paged, const sdsat_paged_batch* batch, const void* d_k,
+                          const void* d_v, const void* d_q, int64_t ld_q, const uint64_t* d_mask,
+                          int32_t window, float scale, void* d_out, int32_t out_dtype, int64_t ld_out);
+
+/* Waits for the handle's stream.  SDSAT_EDATA if a call since the last status met sequences or pages
+ * that do not fit (see sdsat_paged_batch). */
+int sdsat_paged_status(sdsat_paged* paged);
+int sdsat_paged_destroy(sdsat_paged* paged);   /* NULL is accepted */
+/* As sdsat_last_error; with NULL the last failure without a handle. */
+const char* sdsat_paged_last_error(const sdsat_paged* paged);
 
 /* ---- op-level entry points (kernel tests and micro-benchmarks) ---- */
 

@@ -38,8 +38,37 @@ class sdsat_stats(ctypes.Structure):
                 ("decode_ms", ctypes.c_double)]
 
 
+class sdsat_logit_rules(ctypes.Structure):
+    _fields_ = [("d_history", ctypes.c_void_p), ("d_history_len", ctypes.c_void_p), ("d_prompt_len", ctypes.c_void_p),
+                ("history_ld", ctypes.c_int32), ("d_tokens", ctypes.c_void_p), ("d_mask", ctypes.c_void_p),
+                ("d_penalties", ctypes.c_void_p), ("d_bias", ctypes.c_void_p), ("bias_ld", ctypes.c_int64),
+                ("d_allowed", ctypes.c_void_p), ("allowed_ld", ctypes.c_int32)]
+
+
+class sdsat_paged_config(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("max_batch", ctypes.c_int32), ("max_ctx", ctypes.c_int32)]
+
+
+class sdsat_paged_batch(ctypes.Structure):
+    _fields_ = [("d_start", ctypes.c_void_p), ("d_len", ctypes.c_void_p), ("d_pages", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("pages_ld", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("max_q", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class sdsat_rope(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rot_dims", ctypes.c_int32), ("mscale", ctypes.c_float),
+                ("turns", ctypes.c_double * 64)]
+
+
+PAGE = 32
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+
 _VP, _I32, _I64, _F32, _U64, _SZ = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
                                    ctypes.c_uint64, ctypes.c_size_t)
+_F64 = ctypes.c_double
 _SIGNATURES = {
     "sdsat_query_sizes": ([ctypes.POINTER(sdsat_config), ctypes.POINTER(_SZ)], _I32),
     "sdsat_init": ([ctypes.POINTER(sdsat_config), ctypes.POINTER(_VP), _I32, _VP, _SZ, _VP, ctypes.POINTER(_VP)], _I32),
@@ -51,6 +80,17 @@ _SIGNATURES = {
     "sdsat_verify_nucleus": ([_VP, _I32, _I32, _VP, _VP, _F32, _F32, _I32, _U64, _VP, _VP, _VP], _I32),
     "sdsat_forward_block_shared": ([_VP, _I32, _I32, _I32, ctypes.POINTER(_I32), _VP, _VP, _VP], _I32),
     "sdsat_token_logprobs": ([_VP, _I32, _I32, _VP, _VP, _F32, _I32, _VP, _VP, _VP, _VP], _I32),
+    "sdsat_adjust_logits": ([_VP, _I32, _I32, _VP, ctypes.POINTER(sdsat_logit_rules), _VP], _I32),
+    "sdsat_rope_init": ([_I32, _I32, _F64, _I32, _F64, _F64, _F64, _F64, _F32, ctypes.POINTER(sdsat_rope)], _I32),
+    "sdsat_paged_query_sizes": ([ctypes.POINTER(sdsat_paged_config), ctypes.POINTER(_SZ)], _I32),
+    "sdsat_paged_init": ([ctypes.POINTER(sdsat_paged_config), _VP, _SZ, _VP, ctypes.POINTER(_VP)], _I32),
+    "sdsat_paged_append": ([_VP, ctypes.POINTER(sdsat_paged_batch), _VP, _VP, _VP, _I32, _I64, ctypes.POINTER(sdsat_rope),
+                            _VP, _VP, _VP, _F32, _VP, _I64], _I32),
+    "sdsat_paged_attention": ([_VP, ctypes.POINTER(sdsat_paged_batch), _VP, _VP, _VP, _I64, _VP, _I32, _F32, _VP, _I32,
+                               _I64], _I32),
+    "sdsat_paged_status": ([_VP], _I32),
+    "sdsat_paged_destroy": ([_VP], _I32),
+    "sdsat_paged_last_error": ([_VP], ctypes.c_char_p),
     "sdsat_commit_kv": ([_VP, _I32, _I32, _VP, _VP], _I32),
     "sdsat_kv_reorder": ([_VP, _I32, _VP, _I32], _I32),
     "sdsat_cache_ptr": ([_VP, _I32, ctypes.POINTER(_VP), ctypes.POINTER(_VP)], _I32),
@@ -190,6 +230,109 @@ def sdsat_token_logprobs(ctx, batch, q, logits, tokens, temperature, n_top, logp
                          top_logprobs=None):
     _check(lib().sdsat_token_logprobs(ctx, batch, q, _ptr(logits), _ptr(tokens), temperature, n_top, _ptr(logprob),
                                       _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs)), ctx)
+
+
+def logit_rules(history=None, history_len=None, prompt_len=None, tokens=None, mask=None, penalties=None, bias=None,
+                allowed=None) -> sdsat_logit_rules:
+    """Rules for sdsat_adjust_logits from device tensors (kept alive by the result): int32 history [batch, n], history_len
+    and prompt_len [batch], tokens [batch, q]; int64 mask [batch * q]; float32 penalties [3, batch] (repetition, frequency,
+    presence) and bias [V], [1, V] or [batch, V]; int32 allowed [batch * q, words], a bit for each id."""
+    _dense(history, history_len, prompt_len, tokens, mask, penalties, bias, allowed)
+    shared = bias is None or bias.dim() == 1 or bias.shape[0] == 1
+    r = sdsat_logit_rules(_ptr(history), _ptr(history_len), _ptr(prompt_len), 0 if history is None else history.shape[-1],
+                          _ptr(tokens), _ptr(mask), _ptr(penalties), _ptr(bias), 0 if shared else bias.shape[-1],
+                          _ptr(allowed), 0 if allowed is None else allowed.shape[-1])
+    r.tensors = (history, history_len, prompt_len, tokens, mask, penalties, bias, allowed)
+    return r
+
+
+def sdsat_adjust_logits(ctx, batch, q, logits, rules, out):
+    _check(lib().sdsat_adjust_logits(ctx, batch, q, _ptr(logits), ctypes.byref(rules), _ptr(out)), ctx)
+
+
+def _dense(*tensors):
+    for t in tensors:
+        if t is not None and not isinstance(t, int) and not t.is_contiguous():
+            raise ValueError("tensor must be contiguous")
+
+
+def _dtype_code(t):
+    import torch
+    codes = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+    if t.dtype not in codes:
+        raise ValueError("tensor must be float32 or bfloat16")
+    return codes[t.dtype]
+
+
+def _row_stride(t, columns=None):
+    """Elements between rows of a 2-D tensor whose rows are contiguous."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("tensor must be 2-D with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def paged_batch(start, length, pages, rows, max_q, max_len) -> sdsat_paged_batch:
+    """The sequences of a call on a paged cache from int32 device tensors (kept alive by the result): start [batch + 1],
+    length [batch], pages [batch, width]; rows of the call's arrays; host bounds of the new tokens of a sequence and of
+    its slots with them."""
+    _dense(start, length)
+    if start.numel() != length.numel() + 1 or pages.dim() != 2 or pages.shape[0] != length.numel():
+        raise ValueError("start must be [batch + 1], length [batch] and pages [batch, width]")
+    b = sdsat_paged_batch(_ptr(start), _ptr(length), _ptr(pages), length.numel(), _row_stride(pages), rows, max_q, max_len)
+    b.tensors = (start, length, pages)
+    return b
+
+
+def sdsat_rope_init(layout="half", rot_dims=128, base=10000.0, scaling="none", factor=1.0, ctx=0.0, low=1.0, high=4.0,
+                    mscale=1.0) -> sdsat_rope:
+    """Rotary positions (see include/sdsat.h): layout "half" or "interleaved", scaling "none", "linear", "ntk" or
+    "parts"."""
+    r = sdsat_rope()
+    _check(lib().sdsat_rope_init(ROPE_LAYOUTS[layout], rot_dims, base, ROPE_SCALINGS[scaling], factor, ctx, low, high,
+                                 mscale, ctypes.byref(r)))
+    return r
+
+
+def _check_paged(rc, paged):
+    if rc != SDSAT_OK:
+        msg = lib().sdsat_paged_last_error(paged)
+        raise SdsatError(rc, msg.decode() if msg else "")
+
+
+def sdsat_paged_query_sizes(cfg: sdsat_paged_config) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().sdsat_paged_query_sizes(ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def sdsat_paged_init(cfg, workspace, stream=None):
+    out = ctypes.c_void_p()
+    _check(lib().sdsat_paged_init(ctypes.byref(cfg), _ptr(workspace), workspace.numel(), _stream(stream), ctypes.byref(out)))
+    return out
+
+
+def sdsat_paged_append(paged, batch, k, v, x, rope=None, pos=None, q_gain=None, k_gain=None, eps=0.0, q_out=None):
+    """x [rows, (heads + 2 kv_heads) * head_dim] float32 or bfloat16, q_out [rows, heads * head_dim]; rows may be strided."""
+    _dense(k, v, pos, q_gain, k_gain)
+    _check_paged(lib().sdsat_paged_append(paged, ctypes.byref(batch), _ptr(k), _ptr(v), _ptr(x), _dtype_code(x),
+                                          _row_stride(x), None if rope is None else ctypes.byref(rope), _ptr(pos),
+                                          _ptr(q_gain), _ptr(k_gain), eps, _ptr(q_out), _row_stride(q_out)), paged)
+
+
+def sdsat_paged_attention(paged, batch, k, v, q, mask=None, window=0, scale=0.0, out=None):
+    """q [rows, heads * head_dim] in the pool's type, out the same or float32; rows may be strided."""
+    _dense(k, v, mask)
+    _check_paged(lib().sdsat_paged_attention(paged, ctypes.byref(batch), _ptr(k), _ptr(v), _ptr(q), _row_stride(q),
+                                             _ptr(mask), window, scale, _ptr(out), _dtype_code(out), _row_stride(out)),
+                 paged)
+
+
+def sdsat_paged_status(paged):
+    _check_paged(lib().sdsat_paged_status(paged), paged)
+
+
+def sdsat_paged_destroy(paged):
+    _check(lib().sdsat_paged_destroy(paged))
 
 
 def sdsat_kv_reorder(ctx, batch, src, first_slot=0):
@@ -353,6 +496,37 @@ class Context:
         return (view(k, dt, lead + (32 * pages, dh), lead_strides + (dh, 1)),
                 view(v, dt, lead + (pages, 2, 4, 4, dh), lead_strides + (page, 4, 8, 1, 32)),
                 view(sdsat_cache_len_ptr(self.handle), torch.int32, (c.max_batch,), (1,)))
+
+
+class Paged:
+    """A paged-cache handle with its workspace, on the current stream; pool(): tensors for one layer's K and V."""
+
+    def __init__(self, cfg: sdsat_paged_config, device="cuda"):
+        import torch
+        self.cfg = cfg
+        self.workspace = torch.empty(sdsat_paged_query_sizes(cfg), dtype=torch.uint8, device=device)
+        self.stream = torch.cuda.current_stream(device)
+        self.handle = sdsat_paged_init(cfg, self.workspace, self.stream)
+
+    def pool(self):
+        """K [pages, kv_heads, 32, head_dim] and V [pages, kv_heads, head_dim, 32], uninitialised."""
+        import torch
+        c = self.cfg
+        dt = torch.bfloat16 if c.dtype == DTYPE_BF16 else torch.float32
+        dev = self.workspace.device
+        return (torch.empty((c.n_pages, c.n_kv_heads, PAGE, c.head_dim), dtype=dt, device=dev),
+                torch.empty((c.n_pages, c.n_kv_heads, c.head_dim, PAGE), dtype=dt, device=dev))
+
+    def close(self):
+        if getattr(self, "handle", None):
+            sdsat_paged_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 _hip = None

@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsdsat.so")
 SOURCES = ["gemm.hip", "attention.hip", "attention_shared.hip", "verify.hip", "logprobs.hip", "misc.hip", "reorder.hip",
-           "prefill.hip", "prefill_gemm.hip", "noalloc.hip", "api.cpp"]
+           "prefill.hip", "prefill_gemm.hip", "noalloc.hip", "paged_append.hip", "paged_attention.hip", "logit_rules.hip",
+           "api.cpp", "paged_api.cpp"]
 ARCH = "gfx950"
 
 

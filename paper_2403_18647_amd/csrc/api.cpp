@@ -597,6 +597,7 @@ int read_err_flag(sdsat_ctx* c) {
                                     : (h & 4) ? "cache capacity exceeded"
                                     : (h & 16) ? "shared prefix longer than a sequence's committed slots"
                                     : (h & 32) ? "source sequence out of range in a reordering"
+                                    : (h & 64) ? "history length out of range in logit rules"
                                                : "attention launched for a shorter cache than committed");
     }
     return SDSAT_OK;
@@ -843,6 +844,30 @@ int sdsat_token_logprobs(sdsat_ctx* c, int32_t batch, int32_t q, const float* d_
     if (!d_logprob && !d_entropy && !n_top) return SDSAT_OK;
     HIPCHK(c, launch_token_logprobs(d_logits, batch * q, c->D.V, d_tokens, temperature, n_top, d_logprob, d_entropy, d_top_ids,
                                     d_top_logprobs, c->lp_part, c->lp_ctr, c->err_flag, c->stream));
+    return SDSAT_OK;
+}
+
+int sdsat_adjust_logits(sdsat_ctx* c, int32_t batch, int32_t q, const float* d_logits, const sdsat_logit_rules* rules,
+                        float* d_out) {
+    if (!c) return fail(nullptr, SDSAT_EINVAL, "ctx is NULL");
+    const DeviceScope scope(c->device);
+    int rc = check_block_args(c, batch, q);
+    if (rc) return rc;
+    if (!d_logits || !d_out || !rules) return fail(c, SDSAT_EINVAL, "NULL logits, out or rules");
+    const sdsat_logit_rules& r = *rules;
+    if (r.d_history && (!r.d_history_len || r.history_ld < 1)) return fail(c, SDSAT_EINVAL, "history needs history_len and history_ld >= 1");
+    if (r.history_ld >= 1 << 24) return fail(c, SDSAT_EUNSUPPORTED, "histories of 2^24 tokens or more");
+    if (r.d_mask && !r.d_tokens) return fail(c, SDSAT_EINVAL, "mask without tokens");
+    if (r.d_tokens && q > 64) return fail(c, SDSAT_EUNSUPPORTED, "block tokens need q <= 64");
+    if (r.d_bias && r.bias_ld && r.bias_ld < c->D.V) return fail(c, SDSAT_EINVAL, "bias_ld must be 0 (one row for all) or at least V");
+    if (r.d_allowed && r.allowed_ld < (c->D.V + 31) / 32) return fail(c, SDSAT_EINVAL, "allowed_ld must be at least V / 32, rounded up");
+    LogitRuleArgs a{};
+    a.logits = d_logits; a.out = d_out; a.B = batch; a.q = q; a.V = c->D.V;
+    a.history = r.d_history; a.history_len = r.d_history_len; a.prompt_len = r.d_prompt_len; a.history_ld = r.history_ld;
+    a.tokens = r.d_tokens; a.mask = r.d_mask; a.penalties = r.d_penalties;
+    a.bias = r.d_bias; a.bias_ld = r.bias_ld; a.allowed = r.d_allowed; a.allowed_ld = r.allowed_ld;
+    a.err = c->err_flag;
+    HIPCHK(c, launch_logit_rules(a, c->stream));
     return SDSAT_OK;
 }
 

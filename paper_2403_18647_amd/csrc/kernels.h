@@ -185,6 +185,79 @@ hipError_t launch_reorder(int esz, void* kc, void* vc, size_t layer_elems, int n
                           int S_max, int* cache_len, int max_len, const int* src, int first_slot, int* steps, int* err,
                           hipStream_t s);
 
+// ---------------------------------------------------------------- paged cache
+// One pool of pages per layer, K [pages][Hkv][32][Dh] and V [pages][Hkv][Dh][32] (a page's slots permuted, vperm).
+// Sequence b of a call: rows start[b] .. start[b + 1] - 1 of the call, new tokens at slots len[b] .. of its pages.
+// A sequence whose numbers do not fit is left out and flagged (bit 4), a page out of range too (bit 1).
+constexpr int kPage = 32;
+struct PagedSeqs {
+    const int* start;        // [B + 1]
+    const int* len;          // [B]
+    const int* pages;        // [B][pages_ld]
+    int B, pages_ld, rows, max_q, max_len, n_pages;
+    int* err;
+};
+
+// Appending: x = rows q | k | v of H + 2 Hkv heads; rotary turns per position (frequency / 2 pi) of each pair
+constexpr int kMaxPairs = 64;
+struct PagedAppendArgs {
+    PagedSeqs seq;
+    void* kp; void* vp;
+    const void* x; long ldx;
+    void* qout; long ldq;
+    const int* pos;          // [rows] or null: the slot
+    const float* q_gain; const float* k_gain;   // [Dh] or null
+    float eps, mscale;
+    int H, Hkv, interleaved, rot;
+    double turns[kMaxPairs];
+};
+hipError_t launch_paged_append(int dtype, int x_dtype, int head_dim, const PagedAppendArgs& a, hipStream_t s);
+
+// Attention.  Rows of the H / Hkv query heads that share a key head are packed, row i * group + head.  Sequences of up to
+// kPagedFewRows packed rows are cut into parts of per_split pages, counted from slot 0, longer ones into tiles of
+// kPagedTileRows packed rows and each tile's pages into `splits` parts.
+constexpr int kPagedFewRows = 64, kPagedTileRows = 128;
+constexpr int kPagedMaxParts = 64;       // parts of a short chunk, at most
+constexpr int kPagedMaxTileParts = 16;   // parts of a tile, at most
+struct PagedPlan {
+    int per_split, max_parts;            // of the handle
+    int splits, tile_wgs, few_wgs;       // of a call
+};
+struct PagedAttnArgs {
+    PagedSeqs seq;
+    const void* kp; const void* vp;
+    const void* q; long ldq;
+    const uint64_t* mask;    // [rows] or null
+    void* out; long ldo; int out_f32;
+    int H, Hkv, window;      // window 0: none
+    float scale;             // times log2 e
+    int per_split, max_parts, splits, tile_wgs;
+    float* part;             // short chunks' parts [B][Hkv][max_parts][kPagedFewRows][Dh + 4], then the tiles'
+    size_t tile_part;        // where those begin
+    int* counter;            // arrivals, zero between launches: [B][Hkv][kPagedFewRows / 32], then [tile][Hkv]
+};
+// per_split and max_parts: of the configuration alone, so that a row's sums do not follow what else is in its call
+PagedPlan plan_paged(int Hkv, int max_batch, int max_ctx);
+// ... and a call's part of the plan
+void plan_paged_call(PagedPlan& p, int H, int Hkv, int B, int rows, int max_q, int max_len);
+size_t paged_part_floats(const PagedPlan& p, int H, int Hkv, int head_dim, int max_batch, int max_rows, size_t* tile_part);
+size_t paged_counter_ints(int H, int Hkv, int max_batch, int max_rows);
+hipError_t launch_paged_attention(int dtype, int head_dim, const PagedPlan& p, const PagedAttnArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- rules on logits
+// (histories, penalties, biases, allowed ids: see sdsat_logit_rules); any pointer but logits and out may be null
+struct LogitRuleArgs {
+    const float* logits; float* out;
+    int B, q, V;
+    const int* history; const int* history_len; const int* prompt_len; int history_ld;
+    const int* tokens; const uint64_t* mask;
+    const float* penalties;                       // [3][B]
+    const float* bias; long bias_ld;              // bias_ld 0: one row for all
+    const uint32_t* allowed; int allowed_ld;
+    int* err;
+};
+hipError_t launch_logit_rules(const LogitRuleArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- misc kernels
 hipError_t launch_embed(int dtype, const void* embed, int n_rows_emb, int d, const int* tokens, int M,
                         float* x, float* xg, const float* gain, int ldxg, float* ssq, int n_ssq, int* err,

@@ -1,0 +1,755 @@
+// Attention over a paged cache: the rows of a call's chunks (pieces of prompts, draft and verify blocks, single tokens)
+// against the pages of their sequences, whose last slots the chunk itself has filled.
+//
+// For sequence b, query head h and the chunk's row i (at slot s = len_b + i):
+//   O = softmax(scale q [K]^T) [V] over the slots it sees: s - window + 1 .. s, or all below len_b and the chunk's slots of
+//   its mask.  A row that sees nothing gives zeros.
+// The H / Hkv query heads that share a key head are rows of one product: packed row i * group + head.
+//
+// The scores of 32 slots and 32 packed rows are formed as S^T = K Q^T, so that a lane has 16 slots of one row (its row's
+// others are in lane ^ 32), and enter O^T += V^T P^T as they stand: K's rows are read in the order in which V's pages hold
+// their slots.  P is rounded to the cache's type (half a step of bf16, 2^-9 of each weight, on the way to an output that
+// is rounded as coarsely; the row's sum takes the unrounded weights); scores, sums and O are float.  A row keeps a base,
+// in units of log 2, that its weights are 2 to the score above; the base is raised, and O scaled, only when a score passes
+// it by more than kRaise: in most blocks nothing is scaled.
+//
+// Two kinds of workgroup of four waves, in one launch:
+//  * tiles, of chunks of more than kPagedFewRows packed rows: 128 rows, 32 for each wave; two pages at a time go straight
+//    into LDS while the two before are used;
+//  * short chunks, up to kPagedFewRows packed rows: 32 rows and a part of the sequence's pages, which the waves take in
+//    turn; a wave's page goes into its own piece of LDS, K's half while the page before is weighed with V, V's half while
+//    the next scores are formed; no barriers.  The waves' results are joined by log-sum-exp in wave order.
+// A chunk's part is per_split pages from a slot that is a multiple of them, the same for the handle's every call: a row's
+// result does not depend on what else is in its call, nor on the chunk's other rows while there are at most kPagedFewRows
+// packed ones.  Results of parts go to scratch; the workgroup that comes last (an arrival count) joins them in part order.
+#include <algorithm>
+
+#include "paged_device.h"
+
+namespace sdsat {
+
+static constexpr float kRaise = 8.f;
+static constexpr int kWaves = 4;
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef unsigned long long u64;
+
+// acc += A(32 x 16) B(16 x 32): lane l holds A's row and B's column l % 32, contraction indices 8 (l / 32) .. + 7; of the
+// result column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4
+__device__ __forceinline__ void mma32(f32x16_t& acc, const Frag<uint16_t>& a, const Frag<uint16_t>& b) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.v), __builtin_bit_cast(bf16x8_t, b.v), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mma32(f32x16_t& acc, const Frag<float>& a, const Frag<float>& b) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.lo[e], b.lo[e], acc, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.hi[e], b.hi[e], acc, 0, 0, 0);
+}
+
+// A page's K (32 rows of DH) or V (DH rows of 32) in LDS: rows as in memory, their 16-byte chunks exchanged by row, so that
+// a chunk of neighbouring rows lies in different banks.
+template <typename T, int DH>
+struct PageTile {
+    static constexpr int E = (int)sizeof(T), HALF = 32 * DH * E, BLK = 2 * HALF, PIECES = HALF / 1024;
+    template <int RB>
+    __device__ __forceinline__ static int swz(int row) {
+        constexpr int CPR = RB / 16;
+        return RB >= 256 ? row & 15 : (row / (256 / RB)) & (CPR - 1);
+    }
+    // where lane `lane` of the piece's load (1 KiB, linear in LDS) reads in the page's K (RB = DH * E) or V (RB = 32 * E)
+    template <int RB>
+    __device__ __forceinline__ static uint32_t source(int piece, int lane) {
+        constexpr int CPR = RB / 16;
+        const int ch = piece * 64 + lane, row = ch / CPR;
+        return (uint32_t)(row * CPR + ((ch % CPR) ^ swz<RB>(row))) * 16;
+    }
+    template <int RB>
+    __device__ __forceinline__ static Frag<T> frag(const unsigned char* at, int row, int first) {   // 8 elements from chunk `first`
+        Frag<T> f;
+        const unsigned char* r = at + row * RB;
+        const int z = swz<RB>(row);
+        if constexpr (sizeof(T) == 2) {
+            f.v = *reinterpret_cast<const u32x4_t*>(r + ((first ^ z) << 4));
+        } else {
+            f.lo = *reinterpret_cast<const f32x4_t*>(r + ((first ^ z) << 4));
+            f.hi = *reinterpret_cast<const f32x4_t*>(r + (((first + 1) ^ z) << 4));
+        }
+        return f;
+    }
+    // K's row of result row l % 32 (lane l): bits 3 and 4 exchanged, the slots' order in V's pages
+    __device__ __forceinline__ static Frag<T> k(const unsigned char* at, int ks, int lane) {
+        const int r = lane & 31, row = (r & 7) | (r & 8) << 1 | (r & 16) >> 1;
+        return frag<DH * E>(at, row, (16 * ks + 8 * (lane >> 5)) * E / 16);
+    }
+    __device__ __forceinline__ static Frag<T> v(const unsigned char* at, int dt, int s, int lane) {
+        return frag<32 * E>(at, 32 * dt + (lane & 31), 8 * (2 * s + (lane >> 5)) * E / 16);
+    }
+};
+
+__device__ __forceinline__ void to_lds(const unsigned char* src, unsigned char* dst) {   // 16 bytes a lane, dst the wave's
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                     (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+// at most N loads are outstanding; what was read from LDS has arrived
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void wait_lds() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// The slots that a lane's row sees, and those that every row of the wave does.
+struct Sight {
+    int first, last;    // slots of this row (of the tree mask: up to the chunk's end)
+    int len;            // tree: the slots below it
+    uint64_t bits;      // ... and of the chunk's those
+    bool tree;
+    int all_first, all_last;
+    __device__ __forceinline__ bool sees(int slot) const {
+        const bool v = (slot >= first) & (slot <= last);
+        return tree ? v & ((slot < len) | (bool)(bits >> ((slot - len) & 63) & 1)) : v;
+    }
+};
+
+// finite values as they are, others as zero; want 0: that, 1: ones where +inf, 2: where -inf, 3: where NaN
+template <typename T>
+__device__ __forceinline__ Frag<T> select_values(const Frag<T>& f, int want) {
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float v = f.get(j);
+        const bool nan = v != v, inf = !nan && fabsf(v) == INFINITY;
+        const bool hit = want == 1 ? inf && v > 0.f : want == 2 ? inf && v < 0.f : nan;
+        x[j] = want == 0 ? (nan || inf ? 0.f : v) : hit ? 1.f : 0.f;
+    }
+    return Frag<T>::from_f32(x);
+}
+template <typename T>
+__device__ __forceinline__ bool not_finite(const Frag<T>& f) {
+    bool b = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b |= !(fabsf(f.get(j)) < INFINITY);
+    return b;
+}
+
+// A wave's 32 rows: queries, and the running softmax over NB pages at a time.
+template <typename T, int DH, int NB>
+struct RowWave {
+    static constexpr int KS = DH / 16, DT = DH / 32;
+    using P = PageTile<T, DH>;
+    Frag<T> q[KS];
+    f32x16_t o[DT];
+    float base, sum;   // base -inf: nothing seen yet
+
+    __device__ __forceinline__ void clear() {
+        base = -INFINITY;
+        sum = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+    }
+    __device__ __forceinline__ void load_q(const T* row, int lane) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = Frag<T>::load(row + 16 * ks + 8 * (lane >> 5));
+    }
+    __device__ __forceinline__ void scores(f32x16_t& s, const unsigned char* k, int lane) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) mma32(s, P::k(k, ks, lane), q[ks]);
+    }
+    // scores of pages blk .. to weights; masked: some row does not see all of them (pages from `end` on: none does)
+    __device__ __forceinline__ void weigh(const f32x16_t (&s)[NB], Frag<T> (&p)[NB][2], int blk, int end, bool masked, const Sight& see,
+                                          float scale, int lane) {
+        float x[NB][16];
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[n][i] = s[n][i];
+        if (masked) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int slot = 32 * (blk + n) + 16 * (i / 4 % 2) + 8 * (i / 8) + 4 * (lane >> 5) + i % 4;
+                    x[n][i] = ((blk + n < end) & see.sees(slot)) ? x[n][i] : -INFINITY;
+                }
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[n][i]);
+        {
+            const uint32_t u = __float_as_uint(top);
+            const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+            top = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * scale;   // scale > 0
+        }
+        if (__any((top > base + kRaise) | ((base == -INFINITY) & (top > base)))) {
+            const float to = fmaxf(base, top);
+            const float alpha = base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - to);
+            sum *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+            base = to;
+        }
+        const float minus = base == -INFINITY ? 0.f : -base;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            float w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(fmaf(x[n][i], scale, minus));
+                sum += w[i];
+            }
+            p[n][0] = Frag<T>::from_f32(w);
+            p[n][1] = Frag<T>::from_f32(w + 8);
+        }
+    }
+    // O += P V of one page.  Where a row does not see all of the page, values that are not finite must not reach it
+    // through a weight of zero: they are taken out of the product, and infinities and NaN of slots that do count are put in
+    // by products with where they stand.
+    __device__ __forceinline__ void weighted(const Frag<T> (&p)[2], const unsigned char* v, bool masked, int lane) {
+        bool odd = false;
+        if (masked) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) odd |= not_finite(P::v(v, dt, s, lane));
+            odd = __any(odd);
+        }
+        if (!odd) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) mma32(o[dt], P::v(v, dt, s, lane), p[s]);
+            return;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) mma32(o[dt], select_values(P::v(v, dt, s, lane), 0), p[s]);
+#pragma unroll 1
+            for (int want = 1; want < 4; ++want) {
+                f32x16_t d;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) d[i] = 0.f;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) mma32(d, select_values(P::v(v, dt, s, lane), want), p[s]);
+                const float x = want == 1 ? INFINITY : want == 2 ? -INFINITY : NAN;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (d[i] > 0.f) o[dt][i] += x;
+            }
+        }
+    }
+    __device__ __forceinline__ float whole_sum() const {
+        const uint32_t u = __float_as_uint(sum);
+        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+};
+
+template <typename V>
+__device__ __forceinline__ void agent_store(V* p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename V>
+__device__ __forceinline__ V agent_load(const V* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ u64 pack2(float lo, float hi) { return (u64)__float_as_uint(hi) << 32 | __float_as_uint(lo); }
+
+// packed rows row0 .. row0 + rows - 1 of a chunk and key head
+struct Rows { int b, h, row0, rows, group; PagedSeq seq; };
+
+template <typename T, int DH>
+__device__ __forceinline__ const T* q_row(const PagedAttnArgs& a, const Rows& r, int i) {
+    const int p = r.row0 + min(i, r.rows - 1);
+    return reinterpret_cast<const T*>(a.q) + (size_t)(r.seq.start + p / r.group) * a.ldq + (size_t)(r.h * r.group + p % r.group) * DH;
+}
+
+template <typename T, int DH>
+__device__ __forceinline__ void store_row(const PagedAttnArgs& a, const Rows& r, int i, int d, f32x4_t v) {
+    const int p = r.row0 + i;
+    const size_t off = (size_t)(r.seq.start + p / r.group) * a.ldo + (size_t)(r.h * r.group + p % r.group) * DH + d;
+    if (sizeof(T) == 4 || a.out_f32) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + off) = v;
+    else *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + off) = uint2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
+}
+
+template <typename T, int DH>
+__device__ __forceinline__ Sight sight_of(const PagedAttnArgs& a, const Rows& r, int w0, int lane) {
+    Sight s;
+    const int end = r.rows - 1;   // rows past it, and those of a wave that has none, look like the last
+    const int i = (r.row0 + min(w0 + (lane & 31), end)) / r.group;
+    const int i0 = (r.row0 + min(w0, end)) / r.group, i1 = (r.row0 + min(w0 + 31, end)) / r.group;
+    s.tree = a.mask != nullptr;
+    s.len = r.seq.len;
+    s.first = a.window && !s.tree ? max(0, r.seq.len + i - a.window + 1) : 0;
+    s.last = r.seq.len + (s.tree ? r.seq.n - 1 : i);
+    s.bits = s.tree ? a.mask[r.seq.start + i] : 0;
+    s.all_first = a.window && !s.tree ? max(0, r.seq.len + i1 - a.window + 1) : 0;
+    s.all_last = s.tree ? r.seq.len - 1 : r.seq.len + i0;
+    return s;
+}
+
+// Parts 0 .. n - 1 of some rows joined by log-sum-exp in part order: part p's at part + p * stride, [row][DH + 4] with O
+// to the part's base, the base and the sum.
+template <typename T, int DH>
+__device__ void join_parts(const PagedAttnArgs& a, const Rows& r, const float* part, size_t stride, int n, float* smem) {
+    constexpr int D4 = DH / 4;
+    const int tid = threadIdx.x;
+    float2* s_w = reinterpret_cast<float2*>(smem);   // [part][row]
+    __syncthreads();
+    for (int i = tid; i < n * r.rows; i += 64 * kWaves) {
+        const u64 u = agent_load(reinterpret_cast<const u64*>(part + i / r.rows * stride + (size_t)(i % r.rows) * (DH + 4) + DH));
+        s_w[i] = float2{__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32))};
+    }
+    __syncthreads();
+    if (tid < r.rows) {
+        float top = -INFINITY, den = 0.f;
+        for (int p = 0; p < n; ++p) top = fmaxf(top, s_w[p * r.rows + tid].x);
+        for (int p = 0; p < n; ++p) {
+            float2& w = s_w[p * r.rows + tid];
+            w.x = w.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.x - top);
+            den = fmaf(w.x, w.y, den);
+        }
+        const float inv = den == 0.f ? 0.f : 1.0f / den;
+        for (int p = 0; p < n; ++p) s_w[p * r.rows + tid].x *= inv;
+    }
+    __syncthreads();
+    for (int e = tid; e < r.rows * D4; e += 64 * kWaves) {
+        const int i = e / D4, d = e % D4 * 4;
+        const float* src = part + (size_t)i * (DH + 4) + d;
+        f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int p0 = 0; p0 < n; p0 += 8) {
+            u64 u[8][2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {   // past the last: the last again, not used
+                const u64* at = reinterpret_cast<const u64*>(src + (size_t)min(p0 + j, n - 1) * stride);
+                u[j][0] = agent_load(at);
+                u[j][1] = agent_load(at + 1);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (p0 + j < n) {
+                    const float w = s_w[(p0 + j) * r.rows + i].x;
+                    acc[0] = fmaf(w, __uint_as_float((uint32_t)u[j][0]), acc[0]);
+                    acc[1] = fmaf(w, __uint_as_float((uint32_t)(u[j][0] >> 32)), acc[1]);
+                    acc[2] = fmaf(w, __uint_as_float((uint32_t)u[j][1]), acc[2]);
+                    acc[3] = fmaf(w, __uint_as_float((uint32_t)(u[j][1] >> 32)), acc[3]);
+                }
+        }
+        store_row<T, DH>(a, r, i, d, acc);
+    }
+}
+
+template <int DH>
+__device__ __forceinline__ void store_part(float* part, int i, int d, f32x4_t v) {
+    u64* at = reinterpret_cast<u64*>(part + (size_t)i * (DH + 4) + d);
+    agent_store(at, pack2(v[0], v[1]));
+    agent_store(at + 1, pack2(v[2], v[3]));
+}
+
+// This workgroup's part is stored; true for the last of n, which finds all of them.  The count is left at zero.
+__device__ __forceinline__ bool arrive(int* counter, int n) {
+    __shared__ int s_last;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0);   // the stores, which write through, are at their place
+    asm volatile("" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int old = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = old == n - 1;
+        if (s_last) agent_store(counter, 0);
+    }
+    __syncthreads();
+    return s_last;
+}
+
+// Pages lo .. hi - 1 that packed rows row0 .. see between them.
+__device__ __forceinline__ void page_range(const PagedAttnArgs& a, const Rows& r, int& lo, int& hi) {
+    const int i0 = r.row0 / r.group, i1 = (r.row0 + r.rows - 1) / r.group;
+    const bool tree = a.mask != nullptr;
+    lo = a.window && !tree ? max(0, r.seq.len + i0 - a.window + 1) / kPage : 0;
+    hi = (r.seq.len + (tree ? r.seq.n - 1 : i1)) / kPage + 1;
+}
+
+// ------------------------------------------------------------------ short chunks
+// Rows (at most 32) over pages lo .. hi - 1 of part sp (of `parts`, the first being part sp0).
+template <typename T, int DH>
+__device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, int lo, int hi, int sp, int sp0, int parts,
+                                         unsigned char* smem, int wave, int lane) {
+    using P = PageTile<T, DH>;
+    constexpr int DT = DH / 32, QUADS = 4 * DT;
+    RowWave<T, DH, 1> w;
+    w.clear();
+    const Sight see = sight_of<T, DH>(a, r, 0, lane);
+    const int begin = sp * a.per_split;
+    const int from = max(lo, begin), to = min(hi, begin + a.per_split);
+    const int first = begin + (from - begin + 3 - wave) / kWaves * kWaves + wave;   // this wave's first page
+    const int cnt = first < to ? (to - first + kWaves - 1) / kWaves : 0;
+    unsigned char* s_k = smem + wave * P::BLK;
+    unsigned char* s_v = s_k + P::HALF;
+    if (cnt > 0) {
+        const size_t page_bytes = (size_t)a.Hkv * P::HALF;
+        const unsigned char* kb = reinterpret_cast<const unsigned char*>(a.kp) + (size_t)r.h * P::HALF;
+        const unsigned char* vb = reinterpret_cast<const unsigned char*>(a.vp) + (size_t)r.h * P::HALF;
+        uint32_t ko[P::PIECES], vo[P::PIECES];
+#pragma unroll
+        for (int i = 0; i < P::PIECES; ++i) {
+            ko[i] = P::template source<DH * P::E>(i, lane);
+            vo[i] = P::template source<32 * P::E>(i, lane);
+        }
+        int ids = 0;   // lane j: the page of this wave's block j of 64
+        bool bad = false;
+        auto load_ids = [&](int i0) {
+            bool ok = true;
+            if (i0 + lane < cnt) ids = page_of(a.seq, r.b, first + (i0 + lane) * kWaves, ok);
+            bad |= !ok;
+        };
+        auto req = [&](int i, const unsigned char* base, const uint32_t (&off)[P::PIECES], unsigned char* dst) {
+            const unsigned char* src = base + (size_t)__builtin_amdgcn_readlane(ids, i & 63) * page_bytes;
+#pragma unroll
+            for (int p = 0; p < P::PIECES; ++p) to_lds(src + off[p], dst + p * 1024);
+        };
+        load_ids(0);
+        w.load_q(q_row<T, DH>(a, r, lane & 31), lane);
+        req(0, kb, ko, s_k);
+        int id_v = __builtin_amdgcn_readlane(ids, 0);
+        auto req_v = [&]() {
+            const unsigned char* src = vb + (size_t)id_v * page_bytes;
+#pragma unroll
+            for (int p = 0; p < P::PIECES; ++p) to_lds(src + vo[p], s_v + p * 1024);
+        };
+        req_v();
+        for (int i = 0; i < cnt; ++i) {
+            const int blk = first + i * kWaves;
+            const bool more = i + 1 < cnt, masked = 32 * blk + 31 > see.all_last || 32 * blk < see.all_first;
+            f32x16_t s[1];
+            Frag<T> p[1][2];
+            wait_loads<P::PIECES>();   // K; V's are behind
+            w.scores(s[0], s_k, lane);
+            wait_lds();
+            if (more) {
+                if (((i + 1) & 63) == 0) load_ids(i + 1);
+                req(i + 1, kb, ko, s_k);
+                id_v = __builtin_amdgcn_readlane(ids, (i + 1) & 63);
+            }
+            w.weigh(s, p, blk, to, masked, see, a.scale, lane);
+            if (more) wait_loads<P::PIECES>();   // V; the next K's are behind
+            else wait_loads<0>();
+            w.weighted(p[0], s_v, masked, lane);
+            wait_lds();
+            if (more) req_v();
+        }
+        if (bad) atomicOr(a.seq.err, 1);
+    }
+    // the waves' results, in their pieces of LDS, joined in wave order
+    __shared__ float s_base[kWaves][32], s_sum[kWaves][32];
+    f32x4_t* own = reinterpret_cast<f32x4_t*>(smem + wave * P::BLK);
+    static_assert(QUADS * 1024 <= P::BLK, "a wave's O fits its page");
+    const float sum = w.whole_sum();
+    if (lane < 32) {
+        s_base[wave][lane] = w.base;
+        s_sum[wave][lane] = sum;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            own[(dt * 4 + j) * 64 + lane] = f32x4_t{w.o[dt][4 * j], w.o[dt][4 * j + 1], w.o[dt][4 * j + 2], w.o[dt][4 * j + 3]};
+    __syncthreads();
+    const int i = lane & 31;
+    float wt[kWaves], top = -INFINITY, den = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_base[k][i]);
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+        const float m = s_base[k][i];
+        wt[k] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        den = fmaf(wt[k], s_sum[k][i], den);
+    }
+    const size_t stride = (size_t)kPagedFewRows * (DH + 4);
+    float* base = a.part + ((size_t)r.b * a.Hkv + r.h) * a.max_parts * stride + (size_t)r.row0 * (DH + 4);
+    float* mine = base + (sp - sp0) * stride;
+    const float inv = den == 0.f ? 0.f : 1.0f / den;
+    for (int qd = wave; qd < QUADS; qd += kWaves) {
+        f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const f32x4_t v = reinterpret_cast<const f32x4_t*>(smem + k * P::BLK)[qd * 64 + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[e], wt[k], acc[e]);
+        }
+        if (i >= r.rows) continue;
+        const int d = 8 * qd + 4 * (lane >> 5);   // quad 4 dt + j: columns 32 dt + 8 j + 4 (lane / 32)
+        if (parts == 1) {
+            store_row<T, DH>(a, r, i, d, acc * inv);
+        } else {
+            store_part<DH>(mine, i, d, acc);
+            if (qd == 0 && lane < 32) agent_store(reinterpret_cast<u64*>(mine + (size_t)i * (DH + 4) + DH), pack2(top, den));
+        }
+    }
+    if (parts == 1) return;
+    int* counter = a.counter + ((size_t)r.b * a.Hkv + r.h) * (kPagedFewRows / 32) + r.row0 / 32;
+    if (arrive(counter, parts)) join_parts<T, DH>(a, r, base, stride, parts, reinterpret_cast<float*>(smem));
+}
+
+// Workgroup `wg` of `wgs` takes pieces wg, wg + wgs, ... of the short chunks': per sequence its parts, row tiles, key heads.
+template <typename T, int DH>
+__device__ __forceinline__ void few_work(const PagedAttnArgs& a, int wg, int wgs, unsigned char* smem, int wave, int lane) {
+    const int group = a.H / a.Hkv;
+    for (int want = wg;; want += wgs) {
+        int before = 0;
+        Rows r;
+        int lo = 0, hi = 0, sp = 0, sp0 = 0, parts = 0;
+        bool found = false;
+        for (int b0 = 0; b0 < a.seq.B && !found; b0 += 64) {
+            // 64 sequences at a time: their pieces, and the sums up to each
+            const int b = b0 + lane, bc = min(b, a.seq.B - 1);
+            const PagedSeq q = load_seq(a.seq, bc);
+            Rows x{bc, 0, 0, q.n * group, group, q};
+            int l = 0, u = 0, mine = 0, tiles = 0, first = 0;
+            if (b < a.seq.B && q.n > 0 && q.n * (long)group <= kPagedFewRows) {
+                page_range(a, x, l, u);
+                first = l / a.per_split;
+                mine = (u - 1) / a.per_split - first + 1;
+                tiles = (x.rows + 31) / 32;
+            }
+            const int pieces = mine * tiles * a.Hkv;
+            int upto = pieces;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(upto, o, 64);
+                if (lane >= o) upto += v;
+            }
+            const int all = __builtin_amdgcn_readlane(upto, 63);
+            if (want < before + all) {
+                const int at = __popcll(__ballot(before + upto <= want));   // the first lane whose sum passes it
+                const int k = want - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(pieces, at));
+                found = true;
+                r.b = b0 + at;
+                r.group = group;
+                r.seq = PagedSeq{__builtin_amdgcn_readlane(q.start, at), __builtin_amdgcn_readlane(q.n, at),
+                                 __builtin_amdgcn_readlane(q.len, at), true};
+                lo = __builtin_amdgcn_readlane(l, at);
+                hi = __builtin_amdgcn_readlane(u, at);
+                sp0 = __builtin_amdgcn_readlane(first, at);
+                parts = __builtin_amdgcn_readlane(mine, at);
+                const int t = __builtin_amdgcn_readlane(tiles, at);
+                r.h = k % a.Hkv;
+                r.row0 = k / a.Hkv % t * 32;
+                r.rows = min(32, r.seq.n * group - r.row0);
+                sp = sp0 + k / a.Hkv / t;
+            }
+            before += all;
+        }
+        if (!found) return;
+        few_rows<T, DH>(a, r, lo, hi, sp, sp0, parts, smem, wave, lane);
+        __syncthreads();   // smem is free
+    }
+}
+
+// ------------------------------------------------------------------ tiles
+template <typename T, int DH>
+__device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsigned char* smem, int wave, int lane) {
+    using P = PageTile<T, DH>;
+    constexpr int DT = DH / 32, NL = P::PIECES / 2;   // 1 KiB loads of a wave per step and operand
+    const int group = a.H / a.Hkv;
+    const int h = wg % a.Hkv, sp = wg / a.Hkv % a.splits, piece = wg / a.Hkv / a.splits;
+    const int b = __builtin_amdgcn_readfirstlane(seq_of_piece(a.seq, piece, group, kPagedTileRows, 1, lane));
+    Rows r{b, h, 0, 0, group, load_seq(a.seq, b)};
+    if (!r.seq.ok || r.seq.n * (long)group <= kPagedFewRows) return;
+    const int packed = r.seq.n * group, tiles = (packed + kPagedTileRows - 1) / kPagedTileRows;
+    const int nth = piece - piece_begin(r.seq.start, group, kPagedTileRows, 1, b);
+    if (nth < 0 || nth >= tiles) return;
+    r.row0 = (tiles - 1 - nth) * kPagedTileRows;   // the longest first
+    r.rows = min(kPagedTileRows, packed - r.row0);
+    int lo, hi;
+    page_range(a, r, lo, hi);
+    const int per = (hi - lo + a.splits - 1) / a.splits, parts = (hi - lo + per - 1) / per;
+    if (sp >= parts) return;
+    lo += sp * per;
+    hi = min(hi, lo + per);
+    const int w0 = 32 * wave;
+    const Sight see = sight_of<T, DH>(a, r, w0, lane);
+    // pages this wave's rows see
+    int wlo = lo, whi = lo;
+    if (w0 < r.rows) {
+        Rows x = r;
+        x.row0 += w0;
+        x.rows = min(32, r.rows - w0);
+        page_range(a, x, wlo, whi);
+    }
+    RowWave<T, DH, 2> w;
+    w.clear();
+    const size_t page_bytes = (size_t)a.Hkv * P::HALF;
+    const unsigned char* kb = reinterpret_cast<const unsigned char*>(a.kp) + (size_t)h * P::HALF;
+    const unsigned char* vb = reinterpret_cast<const unsigned char*>(a.vp) + (size_t)h * P::HALF;
+    uint32_t ko[NL], vo[NL];   // waves 0, 1 load a step's first page, waves 2, 3 its second, half of K and of V each
+    const int part0 = (wave & 1) * NL;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        ko[i] = P::template source<DH * P::E>(part0 + i, lane);
+        vo[i] = P::template source<32 * P::E>(part0 + i, lane);
+    }
+    int ids = 0;
+    bool bad = false;
+    auto load_ids = [&](int i0) {   // of pages lo + i0 + lane
+        bool ok = true;
+        if (lo + i0 + lane < hi) ids = page_of(a.seq, b, lo + i0 + lane, ok);
+        bad |= !ok;
+    };
+    const int nstep = (hi - lo + 1) / 2;
+    auto request = [&](int i) {   // a page past the last repeats it: in bounds, weighed with nothing
+        if ((i & 31) == 0) load_ids(2 * i);
+        const int j = min(2 * i + (wave >> 1), hi - lo - 1);
+        const size_t off = (size_t)__builtin_amdgcn_readlane(ids, j & 63) * page_bytes;
+        unsigned char* dst = smem + (i & 1) * 2 * P::BLK + (wave >> 1) * P::BLK + part0 * 1024;
+#pragma unroll
+        for (int p = 0; p < NL; ++p) {
+            to_lds(kb + off + ko[p], dst + p * 1024);
+            to_lds(vb + off + vo[p], dst + P::HALF + p * 1024);
+        }
+    };
+    w.load_q(q_row<T, DH>(a, r, w0 + (lane & 31)), lane);
+    request(0);
+    for (int i = 0; i < nstep; ++i) {
+        // this wave's loads of step i have landed; after the barrier everyone's have, and nobody still reads the other stage
+        wait_lds();
+        wait_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (i + 1 < nstep) request(i + 1);
+        const int blk = lo + 2 * i;
+        if (blk >= whi || blk + 2 <= wlo) continue;
+        const unsigned char* st = smem + (i & 1) * 2 * P::BLK;
+        const bool masked = 32 * blk + 63 > see.all_last || 32 * blk < see.all_first || blk + 2 > hi;
+        f32x16_t s[2];
+        Frag<T> p[2][2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) w.scores(s[n], st + n * P::BLK, lane);
+        w.weigh(s, p, blk, hi, masked, see, a.scale, lane);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) w.weighted(p[n], st + n * P::BLK + P::HALF, masked, lane);
+    }
+    if (bad) atomicOr(a.seq.err, 1);
+    const float den = w.whole_sum(), inv = den == 0.f ? 0.f : 1.0f / den;
+    const size_t stride = (size_t)kPagedTileRows * (DH + 4);
+    float* base = a.part + a.tile_part + ((size_t)piece * a.Hkv + h) * a.splits * stride;
+    float* mine = base + sp * stride;
+    const int i = w0 + (lane & 31);
+    if (i < r.rows) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4_t v = f32x4_t{w.o[dt][4 * j], w.o[dt][4 * j + 1], w.o[dt][4 * j + 2], w.o[dt][4 * j + 3]};
+                const int d = 32 * dt + 8 * j + 4 * (lane >> 5);
+                if (parts == 1) store_row<T, DH>(a, r, i, d, v * inv);
+                else store_part<DH>(mine, i, d, v);
+            }
+        if (parts > 1 && lane < 32) agent_store(reinterpret_cast<u64*>(mine + (size_t)i * (DH + 4) + DH), pack2(w.base, den));
+    }
+    if (parts == 1) return;
+    int* counter = a.counter + (size_t)a.seq.B * a.Hkv * (kPagedFewRows / 32) + (size_t)piece * a.Hkv + h;
+    if (arrive(counter, parts)) join_parts<T, DH>(a, r, base, stride, parts, reinterpret_cast<float*>(smem));
+}
+
+template <typename T, int DH, bool TILES>
+__global__ void __launch_bounds__(64 * kWaves, sizeof(T) * DH > 256 ? 1 : 2) paged_attn_kernel(PagedAttnArgs a) {
+    __shared__ __align__(1024) unsigned char smem[kWaves * PageTile<T, DH>::BLK];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (blockIdx.x == 0 && wave == 0) check_seqs(a.seq, lane);
+    if constexpr (TILES) {
+        if ((int)blockIdx.x < a.tile_wgs) {
+            tile_rows<T, DH>(a, (int)blockIdx.x, smem, wave, lane);
+            return;
+        }
+    }
+    few_work<T, DH>(a, (int)blockIdx.x - a.tile_wgs, (int)gridDim.x - a.tile_wgs, smem, wave, lane);
+}
+
+// ------------------------------------------------------------------ plans
+PagedPlan plan_paged(int Hkv, int max_batch, int max_ctx) {
+    PagedPlan p{};
+    const long cap = std::max(1, (max_ctx + kPage - 1) / kPage), pairs = (long)Hkv * max_batch;
+    // pages of a part: a full cache in about 1024 parts, four for each wave at the least
+    long per = std::max<long>(4, std::min<long>((cap * pairs + 1023) / 1024, 64));
+    per = std::max(per, (cap + kPagedMaxParts - 1) / kPagedMaxParts);
+    p.per_split = (int)per;
+    p.max_parts = (int)((cap + per - 1) / per);
+    return p;
+}
+
+static long tile_pieces(int H, int Hkv, long rows, int B) { return rows * (H / Hkv) / kPagedTileRows + B; }
+
+// parts of a tile's pages: as many as fill the compute units twice
+static int tile_splits(long pieces, int Hkv) { return (int)std::max<long>(1, std::min<long>(kPagedMaxTileParts, 512 / (pieces * Hkv))); }
+
+void plan_paged_call(PagedPlan& p, int H, int Hkv, int B, int rows, int max_q, int max_len) {
+    const int group = H / Hkv;
+    p.splits = 1;
+    p.tile_wgs = 0;
+    if ((long)max_q * group > kPagedFewRows) {
+        const long pieces = tile_pieces(H, Hkv, rows, B);
+        p.splits = std::min(tile_splits(pieces, Hkv), (max_len + 4 * kPage - 1) / (4 * kPage));
+        p.tile_wgs = (int)std::min<long>(pieces * Hkv * p.splits, 0x7FFFFFFF);
+    }
+    const int tiles = (int)std::min<long>(((long)max_q * group + 31) / 32, kPagedFewRows / 32);
+    const long parts = ((long)max_len + kPage * p.per_split - 1) / (kPage * p.per_split);
+    p.few_wgs = (int)std::max<long>(1, std::min<long>(parts * B * tiles * Hkv, 2048));
+}
+
+size_t paged_part_floats(const PagedPlan& p, int H, int Hkv, int head_dim, int max_batch, int max_rows, size_t* tile_part) {
+    const size_t few = p.max_parts > 1 ? (size_t)max_batch * Hkv * p.max_parts * kPagedFewRows * (head_dim + 4) : 0;
+    // pieces * Hkv * splits <= 512 wherever splits > 1; where there are fewer pieces, splits are bounded
+    *tile_part = few;
+    return few + ((long)max_rows * (H / Hkv) > kPagedFewRows ? (size_t)512 * kPagedTileRows * (head_dim + 4) : 0);
+}
+
+size_t paged_counter_ints(int H, int Hkv, int max_batch, int max_rows) {
+    return (size_t)max_batch * Hkv * (kPagedFewRows / 32) + (size_t)tile_pieces(H, Hkv, max_rows, max_batch) * Hkv;
+}
+
+template <typename T, int DH>
+static hipError_t launch_dh(const PagedPlan& p, const PagedAttnArgs& a, hipStream_t s) {
+    const unsigned grid = (unsigned)p.tile_wgs + (unsigned)p.few_wgs;
+    if (p.tile_wgs)
+        hipLaunchKernelGGL((paged_attn_kernel<T, DH, true>), dim3(grid), dim3(64 * kWaves), 0, s, a);
+    else
+        hipLaunchKernelGGL((paged_attn_kernel<T, DH, false>), dim3(grid), dim3(64 * kWaves), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_attention(int dtype, int head_dim, const PagedPlan& p, const PagedAttnArgs& a, hipStream_t s) {
+    const PagedSeqs& q = a.seq;
+    const int group = a.Hkv > 0 ? a.H / a.Hkv : 0;
+    if (group < 1 || a.H % a.Hkv || q.B < 1 || q.rows < 0 || q.pages_ld < 1 || q.n_pages < 1 || q.max_q < 0 || q.max_len < 0 ||
+        q.max_len > (long)q.pages_ld * kPage || !q.start || !q.len || !q.pages || !q.err || !a.kp || !a.vp || !a.q || !a.out ||
+        (a.mask && (q.max_q > 64 || a.window)) || a.window < 0 || !(a.scale > 0.f) || a.ldq % 8 || a.ldo % 4 || p.per_split < 1 ||
+        a.per_split != p.per_split || a.splits != p.splits || a.tile_wgs != p.tile_wgs || a.max_parts != p.max_parts ||
+        p.splits < 1 || p.splits > kPagedMaxTileParts || p.few_wgs < 1 || p.max_parts > kPagedMaxParts ||
+        (long)p.tile_wgs + p.few_wgs > 0x7FFFFFFFl / (64 * kWaves) || q.max_len > (long)p.max_parts * p.per_split * kPage ||
+        (long)p.max_parts * p.per_split > 0x7FFFFFFFl / kPage || !a.part || !a.counter ||
+        (p.tile_wgs && p.tile_wgs != tile_pieces(a.H, a.Hkv, q.rows, q.B) * a.Hkv * p.splits) ||
+        ((long)q.max_q * group > kPagedFewRows && !p.tile_wgs) ||
+        (p.splits > 1 && tile_pieces(a.H, a.Hkv, q.rows, q.B) * a.Hkv * p.splits > 512))
+        return hipErrorInvalidValue;
+    if (dtype == 1) {
+        if (head_dim == 128) return launch_dh<uint16_t, 128>(p, a, s);
+        if (head_dim == 64) return launch_dh<uint16_t, 64>(p, a, s);
+    } else {
+        if (head_dim == 128) return launch_dh<float, 128>(p, a, s);
+        if (head_dim == 64) return launch_dh<float, 64>(p, a, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace sdsat
