@@ -54,7 +54,7 @@ struct PageTile {
     template <int RB>
     __device__ __forceinline__ static int swz(int row) {
         constexpr int CPR = RB / 16;
-        return RB >= 256 ? row & 15 : (row / (256 / RB)) & (CPR - 1);
+        return RB >= 256 ? row & 15 : (row * RB / 256) & (CPR - 1);
     }
     // where lane `lane` of the piece's load (1 KiB, linear in LDS) reads in the page's K (RB = DH * E) or V (RB = 32 * E)
     template <int RB>
@@ -86,10 +86,103 @@ struct PageTile {
     }
 };
 
-__device__ __forceinline__ void to_lds(const unsigned char* src, unsigned char* dst) {   // 16 bytes a lane, dst the wave's
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                     (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+// A page's K or V on its way into LDS (at dst, the wave's), through a buffer resource over it: the pieces' addresses repeat
+// after 16 rows, so a few lane offsets and the instruction's own offset (which counts on both sides) make them.
+template <typename T, int DH, int RB>
+struct Fetch {
+    using P = PageTile<T, DH>;
+    static constexpr int VARS = RB / 64;
+    uint32_t off[VARS];
+    __device__ __forceinline__ explicit Fetch(int lane) {
+#pragma unroll
+        for (int i = 0; i < VARS; ++i) off[i] = P::template source<RB>(i, lane) - i * 1024;
+    }
+    template <int N, int I = 0>   // pieces first .. first + N - 1 (first a multiple of VARS), to their places
+    __device__ __forceinline__ void pieces(const unsigned char* src, unsigned char* dst, int first) const {
+        if constexpr (I < N) {
+            const int at = (first + I / 4 * 4) * 1024;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_rsrc(src, P::HALF), (__attribute__((address_space(3))) void*)(dst + at), 16,
+                                                     off[I % VARS], at, I % 4 * 1024, 0);
+            pieces<N, I + 1>(src, dst, first);
+        }
+    }
+};
+// Eight fragments out of LDS, and the wait for them.  In one piece of assembly: the compiler holds every read of LDS behind
+// all loads into it that are in flight, the ones for the next page too.
+template <int O0, int O1, int O2, int O3, int O4, int O5, int O6, int O7>
+__device__ __forceinline__ void read8(Frag<uint16_t> (&f)[8], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t a4,
+                                      uint32_t a5, uint32_t a6, uint32_t a7) {
+    asm volatile(
+        "ds_read_b128 %0, %8 offset:%16\n\tds_read_b128 %1, %9 offset:%17\n\tds_read_b128 %2, %10 offset:%18\n\t"
+        "ds_read_b128 %3, %11 offset:%19\n\tds_read_b128 %4, %12 offset:%20\n\tds_read_b128 %5, %13 offset:%21\n\t"
+        "ds_read_b128 %6, %14 offset:%22\n\tds_read_b128 %7, %15 offset:%23\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(f[0].v), "=&v"(f[1].v), "=&v"(f[2].v), "=&v"(f[3].v), "=&v"(f[4].v), "=&v"(f[5].v), "=&v"(f[6].v), "=&v"(f[7].v)
+        : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(a4), "v"(a5), "v"(a6), "v"(a7), "i"(O0), "i"(O1), "i"(O2), "i"(O3), "i"(O4),
+          "i"(O5), "i"(O6), "i"(O7)
+        : "memory");
 }
+template <int O0, int O1, int O2, int O3>
+__device__ __forceinline__ void read4(Frag<uint16_t> (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+    asm volatile(
+        "ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%9\n\tds_read_b128 %2, %6 offset:%10\n\t"
+        "ds_read_b128 %3, %7 offset:%11\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(f[0].v), "=&v"(f[1].v), "=&v"(f[2].v), "=&v"(f[3].v)
+        : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "i"(O0), "i"(O1), "i"(O2), "i"(O3)
+        : "memory");
+}
+// A lane's reads of a page in LDS, K at `base` (bytes into smem), V behind it: all fragments of a head, and the wait.
+template <typename T, int DH>
+struct PageRead {
+    using P = PageTile<T, DH>;
+    static constexpr int KS = DH / 16, DT = DH / 32;
+    const unsigned char* at;
+    int lane;
+    __device__ __forceinline__ PageRead(const unsigned char* smem, int base, int l) : at(smem + base), lane(l) {}
+    __device__ __forceinline__ void move(int by) { at += by; }
+    template <int AT>   // the page AT bytes further
+    __device__ __forceinline__ void k(Frag<T> (&f)[KS]) const {
+#pragma unroll
+        for (int i = 0; i < KS; ++i) f[i] = P::k(at + AT, i, lane);
+    }
+    template <int AT>   // fragment s * DT + dt
+    __device__ __forceinline__ void v(Frag<T> (&f)[KS]) const {
+#pragma unroll
+        for (int i = 0; i < KS; ++i) f[i] = P::v(at + AT + P::HALF, i % DT, i / DT, lane);
+    }
+};
+template <int DH>
+struct PageRead<uint16_t, DH> {
+    using P = PageTile<uint16_t, DH>;
+    static constexpr int KS = DH / 16;
+    uint32_t ka[KS], va[2];
+    __device__ __forceinline__ PageRead(const unsigned char* smem, int base, int lane) {
+        const uint32_t at = (uint32_t)(size_t)(const __attribute__((address_space(3))) unsigned char*)smem + base;
+        const int r = lane & 31, g = lane >> 5, row = (r & 7) | (r & 8) << 1 | (r & 16) >> 1;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) ka[ks] = at + row * DH * 2 + ((2 * ks + g) ^ P::template swz<DH * 2>(row)) * 16;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) va[s] = at + P::HALF + r * 64 + ((2 * s + g) ^ P::template swz<64>(r)) * 16;
+    }
+    __device__ __forceinline__ void move(int by) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) ka[ks] += by;
+        va[0] += by;
+        va[1] += by;
+    }
+    template <int AT>
+    __device__ __forceinline__ void k(Frag<uint16_t> (&f)[KS]) const {
+        if constexpr (KS == 8) read8<AT, AT, AT, AT, AT, AT, AT, AT>(f, ka[0], ka[1], ka[2], ka[3], ka[4], ka[5], ka[6], ka[7]);
+        else read4<AT, AT, AT, AT>(f, ka[0], ka[1], ka[2], ka[3]);
+    }
+    template <int AT>
+    __device__ __forceinline__ void v(Frag<uint16_t> (&f)[KS]) const {
+        if constexpr (KS == 8)
+            read8<AT, AT + 2048, AT + 4096, AT + 6144, AT, AT + 2048, AT + 4096, AT + 6144>(f, va[0], va[0], va[0], va[0], va[1], va[1], va[1], va[1]);
+        else
+            read4<AT, AT + 2048, AT, AT + 2048>(f, va[0], va[0], va[1], va[1]);
+    }
+};
+
 // at most N loads are outstanding; what was read from LDS has arrived
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -121,7 +214,10 @@ struct Sight {
 
 // finite values as they are, others as zero; want 0: that, 1: ones where +inf, 2: where -inf, 3: where NaN
 template <typename T>
-__device__ __forceinline__ Frag<T> select_values(const Frag<T>& f, int want) {
+__device__ __forceinline__ Frag<T> select_values(Frag<T> f, int want) {
+    // opaque: nothing of this is formed ahead for the steps that do not need it
+    if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(f.v));
+    else asm volatile("" : "+v"(f.lo), "+v"(f.hi));
     float x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -132,8 +228,13 @@ __device__ __forceinline__ Frag<T> select_values(const Frag<T>& f, int want) {
     }
     return Frag<T>::from_f32(x);
 }
-template <typename T>
-__device__ __forceinline__ bool not_finite(const Frag<T>& f) {
+__device__ __forceinline__ bool not_finite(const Frag<uint16_t>& f) {   // all ones in an exponent
+    bool b = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b |= ((f.v[j] & 0x7F80u) == 0x7F80u) | ((f.v[j] & 0x7F800000u) == 0x7F800000u);
+    return b;
+}
+__device__ __forceinline__ bool not_finite(const Frag<float>& f) {
     bool b = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) b |= !(fabsf(f.get(j)) < INFINITY);
@@ -144,7 +245,6 @@ __device__ __forceinline__ bool not_finite(const Frag<T>& f) {
 template <typename T, int DH, int NB>
 struct RowWave {
     static constexpr int KS = DH / 16, DT = DH / 32;
-    using P = PageTile<T, DH>;
     Frag<T> q[KS];
     f32x16_t o[DT];
     float base, sum;   // base -inf: nothing seen yet
@@ -161,11 +261,20 @@ struct RowWave {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) q[ks] = Frag<T>::load(row + 16 * ks + 8 * (lane >> 5));
     }
-    __device__ __forceinline__ void scores(f32x16_t& s, const unsigned char* k, int lane) const {
+    // the queries are here: their loads, ahead of those into LDS, are waited for once and not in every step
+    __device__ __forceinline__ void have_q() {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(q[ks].v));
+            else asm volatile("" : "+v"(q[ks].lo), "+v"(q[ks].hi));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __device__ __forceinline__ void scores(f32x16_t& s, const Frag<T> (&k)[KS]) const {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) mma32(s, P::k(k, ks, lane), q[ks]);
+        for (int ks = 0; ks < KS; ++ks) mma32(s, k[ks], q[ks]);
     }
     // scores of pages blk .. to weights; masked: some row does not see all of them (pages from `end` on: none does)
     __device__ __forceinline__ void weigh(const f32x16_t (&s)[NB], Frag<T> (&p)[NB][2], int blk, int end, bool masked, const Sight& see,
@@ -218,39 +327,43 @@ struct RowWave {
     // O += P V of one page.  Where a row does not see all of the page, values that are not finite must not reach it
     // through a weight of zero: they are taken out of the product, and infinities and NaN of slots that do count are put in
     // by products with where they stand.
-    __device__ __forceinline__ void weighted(const Frag<T> (&p)[2], const unsigned char* v, bool masked, int lane) {
+    __device__ __forceinline__ void weighted(const Frag<T> (&p)[2], Frag<T> (&v)[KS], bool masked) {
         bool odd = false;
         if (masked) {
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) odd |= not_finite(P::v(v, dt, s, lane));
+            for (int i = 0; i < KS; ++i) odd |= not_finite(v[i]);
             odd = __any(odd);
         }
-        if (!odd) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) mma32(o[dt], P::v(v, dt, s, lane), p[s]);
-            return;
-        }
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) mma32(o[dt], select_values(P::v(v, dt, s, lane), 0), p[s]);
+        if (odd) {
+            // one copy of this, on tile 0, the tiles taking turns there
 #pragma unroll 1
-            for (int want = 1; want < 4; ++want) {
-                f32x16_t d;
+            for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll 1
+                for (int want = 1; want < 4; ++want) {
+                    f32x16_t d;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) d[i] = 0.f;
+                    for (int i = 0; i < 16; ++i) d[i] = 0.f;
 #pragma unroll
-                for (int s = 0; s < 2; ++s) mma32(d, select_values(P::v(v, dt, s, lane), want), p[s]);
-                const float x = want == 1 ? INFINITY : want == 2 ? -INFINITY : NAN;
+                    for (int s = 0; s < 2; ++s) mma32(d, select_values(v[s * DT], want), p[s]);
+                    const float x = want == 1 ? INFINITY : want == 2 ? -INFINITY : NAN;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (d[i] > 0.f) o[dt][i] += x;
+                    for (int i = 0; i < 16; ++i) o[0][i] += d[i] > 0.f ? x : 0.f;
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const Frag<T> f = select_values(v[s * DT], 0);
+#pragma unroll
+                    for (int t = 0; t + 1 < DT; ++t) v[s * DT + t] = v[s * DT + t + 1];
+                    v[s * DT + DT - 1] = f;
+                }
+                const f32x16_t o0 = o[0];
+#pragma unroll
+                for (int t = 0; t + 1 < DT; ++t) o[t] = o[t + 1];
+                o[DT - 1] = o0;
             }
         }
+#pragma unroll
+        for (int i = 0; i < KS; ++i) mma32(o[i % DT], v[i], p[i / DT]);
     }
     __device__ __forceinline__ float whole_sum() const {
         const uint32_t u = __float_as_uint(sum);
@@ -400,12 +513,8 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
         const size_t page_bytes = (size_t)a.Hkv * P::HALF;
         const unsigned char* kb = reinterpret_cast<const unsigned char*>(a.kp) + (size_t)r.h * P::HALF;
         const unsigned char* vb = reinterpret_cast<const unsigned char*>(a.vp) + (size_t)r.h * P::HALF;
-        uint32_t ko[P::PIECES], vo[P::PIECES];
-#pragma unroll
-        for (int i = 0; i < P::PIECES; ++i) {
-            ko[i] = P::template source<DH * P::E>(i, lane);
-            vo[i] = P::template source<32 * P::E>(i, lane);
-        }
+        const Fetch<T, DH, DH * P::E> fk(lane);
+        const Fetch<T, DH, 32 * P::E> fv(lane);
         int ids = 0;   // lane j: the page of this wave's block j of 64
         bool bad = false;
         auto load_ids = [&](int i0) {
@@ -413,40 +522,36 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
             if (i0 + lane < cnt) ids = page_of(a.seq, r.b, first + (i0 + lane) * kWaves, ok);
             bad |= !ok;
         };
-        auto req = [&](int i, const unsigned char* base, const uint32_t (&off)[P::PIECES], unsigned char* dst) {
-            const unsigned char* src = base + (size_t)__builtin_amdgcn_readlane(ids, i & 63) * page_bytes;
-#pragma unroll
-            for (int p = 0; p < P::PIECES; ++p) to_lds(src + off[p], dst + p * 1024);
-        };
         load_ids(0);
         w.load_q(q_row<T, DH>(a, r, lane & 31), lane);
-        req(0, kb, ko, s_k);
-        int id_v = __builtin_amdgcn_readlane(ids, 0);
-        auto req_v = [&]() {
-            const unsigned char* src = vb + (size_t)id_v * page_bytes;
-#pragma unroll
-            for (int p = 0; p < P::PIECES; ++p) to_lds(src + vo[p], s_v + p * 1024);
-        };
-        req_v();
+        __builtin_amdgcn_sched_barrier(0);
+        int id = __builtin_amdgcn_readlane(ids, 0);
+        fk.template pieces<P::PIECES>(kb + (size_t)id * page_bytes, s_k, 0);
+        fv.template pieces<P::PIECES>(vb + (size_t)id * page_bytes, s_v, 0);
+        w.have_q();
+        const PageRead<T, DH> rd(smem, wave * P::BLK, lane);
         for (int i = 0; i < cnt; ++i) {
             const int blk = first + i * kWaves;
             const bool more = i + 1 < cnt, masked = 32 * blk + 31 > see.all_last || 32 * blk < see.all_first;
             f32x16_t s[1];
             Frag<T> p[1][2];
             wait_loads<P::PIECES>();   // K; V's are behind
-            w.scores(s[0], s_k, lane);
-            wait_lds();
+            Frag<T> f[DH / 16];
+            rd.template k<0>(f);
+            if constexpr (sizeof(T) == 4) wait_lds();
             if (more) {
                 if (((i + 1) & 63) == 0) load_ids(i + 1);
-                req(i + 1, kb, ko, s_k);
-                id_v = __builtin_amdgcn_readlane(ids, (i + 1) & 63);
+                id = __builtin_amdgcn_readlane(ids, (i + 1) & 63);
+                fk.template pieces<P::PIECES>(kb + (size_t)id * page_bytes, s_k, 0);
             }
+            w.scores(s[0], f);
             w.weigh(s, p, blk, to, masked, see, a.scale, lane);
             if (more) wait_loads<P::PIECES>();   // V; the next K's are behind
             else wait_loads<0>();
-            w.weighted(p[0], s_v, masked, lane);
-            wait_lds();
-            if (more) req_v();
+            rd.template v<0>(f);
+            if constexpr (sizeof(T) == 4) wait_lds();
+            if (more) fv.template pieces<P::PIECES>(vb + (size_t)id * page_bytes, s_v, 0);
+            w.weighted(p[0], f, masked);
         }
         if (bad) atomicOr(a.seq.err, 1);
     }
@@ -592,13 +697,10 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
     const size_t page_bytes = (size_t)a.Hkv * P::HALF;
     const unsigned char* kb = reinterpret_cast<const unsigned char*>(a.kp) + (size_t)h * P::HALF;
     const unsigned char* vb = reinterpret_cast<const unsigned char*>(a.vp) + (size_t)h * P::HALF;
-    uint32_t ko[NL], vo[NL];   // waves 0, 1 load a step's first page, waves 2, 3 its second, half of K and of V each
+    // waves 0, 1 load a step's first page, waves 2, 3 its second, half of K and of V each
     const int part0 = (wave & 1) * NL;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        ko[i] = P::template source<DH * P::E>(part0 + i, lane);
-        vo[i] = P::template source<32 * P::E>(part0 + i, lane);
-    }
+    const Fetch<T, DH, DH * P::E> fk(lane);
+    const Fetch<T, DH, 32 * P::E> fv(lane);
     int ids = 0;
     bool bad = false;
     auto load_ids = [&](int i0) {   // of pages lo + i0 + lane
@@ -611,15 +713,15 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
         if ((i & 31) == 0) load_ids(2 * i);
         const int j = min(2 * i + (wave >> 1), hi - lo - 1);
         const size_t off = (size_t)__builtin_amdgcn_readlane(ids, j & 63) * page_bytes;
-        unsigned char* dst = smem + (i & 1) * 2 * P::BLK + (wave >> 1) * P::BLK + part0 * 1024;
-#pragma unroll
-        for (int p = 0; p < NL; ++p) {
-            to_lds(kb + off + ko[p], dst + p * 1024);
-            to_lds(vb + off + vo[p], dst + P::HALF + p * 1024);
-        }
+        unsigned char* dst = smem + (i & 1) * 2 * P::BLK + (wave >> 1) * P::BLK;
+        fk.template pieces<NL>(kb + off, dst, part0);
+        fv.template pieces<NL>(vb + off, dst + P::HALF, part0);
     };
     w.load_q(q_row<T, DH>(a, r, w0 + (lane & 31)), lane);
+    __builtin_amdgcn_sched_barrier(0);
     request(0);
+    w.have_q();
+    PageRead<T, DH> rd(smem, 0, lane);
     for (int i = 0; i < nstep; ++i) {
         // this wave's loads of step i have landed; after the barrier everyone's have, and nobody still reads the other stage
         wait_lds();
@@ -628,16 +730,21 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
         asm volatile("" ::: "memory");
         if (i + 1 < nstep) request(i + 1);
         const int blk = lo + 2 * i;
-        if (blk >= whi || blk + 2 <= wlo) continue;
-        const unsigned char* st = smem + (i & 1) * 2 * P::BLK;
-        const bool masked = 32 * blk + 63 > see.all_last || 32 * blk < see.all_first || blk + 2 > hi;
-        f32x16_t s[2];
-        Frag<T> p[2][2];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) w.scores(s[n], st + n * P::BLK, lane);
-        w.weigh(s, p, blk, hi, masked, see, a.scale, lane);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) w.weighted(p[n], st + n * P::BLK + P::HALF, masked, lane);
+        if (blk < whi && blk + 2 > wlo) {
+            const bool masked = 32 * blk + 63 > see.all_last || 32 * blk < see.all_first || blk + 2 > hi;
+            f32x16_t s[2];
+            Frag<T> p[2][2], f[DH / 16];
+            rd.template k<0>(f);
+            w.scores(s[0], f);
+            rd.template k<P::BLK>(f);
+            w.scores(s[1], f);
+            w.weigh(s, p, blk, hi, masked, see, a.scale, lane);
+            rd.template v<0>(f);
+            w.weighted(p[0], f, masked);
+            rd.template v<P::BLK>(f);
+            w.weighted(p[1], f, masked);
+        }
+        rd.move(i & 1 ? -2 * P::BLK : 2 * P::BLK);
     }
     if (bad) atomicOr(a.seq.err, 1);
     const float den = w.whole_sum(), inv = den == 0.f ? 0.f : 1.0f / den;
