@@ -215,13 +215,14 @@ hipError_t launch_paged_append(int dtype, int x_dtype, int head_dim, const Paged
 
 // Attention.  Rows of the H / Hkv query heads that share a key head are packed, row i * group + head.  Sequences of up to
 // kPagedFewRows packed rows are cut into parts of per_split pages, counted from slot 0, longer ones into tiles of
-// kPagedTileRows packed rows and each tile's pages into `splits` parts.
+// kPagedTileRows packed rows, and each tile's pages into parts where there are few tiles.
 constexpr int kPagedFewRows = 64, kPagedTileRows = 128;
 constexpr int kPagedMaxParts = 64;       // parts of a short chunk, at most
 constexpr int kPagedMaxTileParts = 16;   // parts of a tile, at most
+constexpr int kPagedTileParts = 512;    // of all tiles and key heads, at most, where tiles have several
 struct PagedPlan {
     int per_split, max_parts;            // of the handle
-    int splits, tile_wgs, few_wgs;       // of a call
+    int tile_wgs, few_wgs, call_parts;   // of a call: workgroups; parts of a short chunk, at most
 };
 struct PagedAttnArgs {
     PagedSeqs seq;
@@ -231,17 +232,15 @@ struct PagedAttnArgs {
     void* out; long ldo; int out_f32;
     int H, Hkv, window;      // window 0: none
     float scale;             // times log2 e
-    int per_split, max_parts, splits, tile_wgs;
+    int per_split, max_parts, tile_wgs, few_wgs;
     float* part;             // short chunks' parts [B][Hkv][max_parts][kPagedFewRows][Dh + 4], then the tiles'
     size_t tile_part;        // where those begin
-    int* counter;            // arrivals, zero between launches: [B][Hkv][kPagedFewRows / 32], then [tile][Hkv]
 };
 // per_split and max_parts: of the configuration alone, so that a row's sums do not follow what else is in its call
 PagedPlan plan_paged(int Hkv, int max_batch, int max_ctx);
 // ... and a call's part of the plan
 void plan_paged_call(PagedPlan& p, int H, int Hkv, int B, int rows, int max_q, int max_len);
 size_t paged_part_floats(const PagedPlan& p, int H, int Hkv, int head_dim, int max_batch, int max_rows, size_t* tile_part);
-size_t paged_counter_ints(int H, int Hkv, int max_batch, int max_rows);
 hipError_t launch_paged_attention(int dtype, int head_dim, const PagedPlan& p, const PagedAttnArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------- rules on logits

@@ -18,7 +18,6 @@ struct sdsat_paged {
     int device = 0;
     std::string err = "no error";
     int* err_flag = nullptr;
-    int* counter = nullptr;
     float* part = nullptr;
     size_t tile_part = 0;
 };
@@ -66,13 +65,11 @@ int check_config(const sdsat_paged_config* c, std::string* why) {
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // Offsets of the workspace's arrays and its size.
-struct Layout { size_t counter, part, bytes, counter_ints, tile_part; PagedPlan plan; };
+struct Layout { size_t part, bytes, tile_part; PagedPlan plan; };
 Layout layout(const sdsat_paged_config& c) {
     Layout l{};
     l.plan = plan_paged(c.n_kv_heads, c.max_batch, c.max_ctx);
-    l.counter = 256;   // ahead of it the error flags
-    l.counter_ints = paged_counter_ints(c.n_heads, c.n_kv_heads, c.max_batch, c.max_rows);
-    l.part = l.counter + align_up(l.counter_ints * 4);
+    l.part = 256;   // ahead of it the error flags
     l.bytes = l.part + align_up(4 * (4 + paged_part_floats(l.plan, c.n_heads, c.n_kv_heads, c.head_dim, c.max_batch, c.max_rows, &l.tile_part)));
     return l;
 }
@@ -153,10 +150,9 @@ int sdsat_paged_init(const sdsat_paged_config* cfg, void* workspace, size_t work
     (void)hipGetDevice(&p->device);
     char* w = static_cast<char*>(workspace);
     p->err_flag = reinterpret_cast<int*>(w);
-    p->counter = reinterpret_cast<int*>(w + l.counter);
     p->part = reinterpret_cast<float*>(w + l.part);
     p->tile_part = l.tile_part;
-    const hipError_t e = launch_fill_i32(p->err_flag, l.counter / 4 + l.counter_ints, 0, p->stream);
+    const hipError_t e = launch_fill_i32(p->err_flag, 1, 0, p->stream);
     if (e != hipSuccess || hipStreamSynchronize(p->stream) != hipSuccess) {
         delete p;
         return fail(nullptr, SDSAT_EDEVICE, "clearing the workspace failed");
@@ -226,8 +222,8 @@ int sdsat_paged_attention(sdsat_paged* p, const sdsat_paged_batch* batch, const 
     a.kp = d_k; a.vp = d_v; a.q = d_q; a.ldq = ld_q; a.mask = d_mask; a.out = d_out; a.ldo = ld_out;
     a.out_f32 = out_dtype == SDSAT_DTYPE_FP32;
     a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.window = window; a.scale = in2;
-    a.per_split = plan.per_split; a.max_parts = plan.max_parts; a.splits = plan.splits; a.tile_wgs = plan.tile_wgs;
-    a.part = p->part; a.tile_part = p->tile_part; a.counter = p->counter;
+    a.per_split = plan.per_split; a.max_parts = plan.max_parts; a.tile_wgs = plan.tile_wgs; a.few_wgs = plan.few_wgs;
+    a.part = p->part; a.tile_part = p->tile_part;
     return launched(p, launch_paged_attention(c.dtype, c.head_dim, plan, a, p->stream), "paged attention");
 }
 

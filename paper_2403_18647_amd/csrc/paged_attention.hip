@@ -21,18 +21,25 @@
 //    the next scores are formed; no barriers.  The waves' results are joined by log-sum-exp in wave order.
 // A chunk's part is per_split pages from a slot that is a multiple of them, the same for the handle's every call: a row's
 // result does not depend on what else is in its call, nor on the chunk's other rows while there are at most kPagedFewRows
-// packed ones.  Results of parts go to scratch; the workgroup that comes last (an arrival count) joins them in part order.
+// packed ones.  Results of parts go to scratch; a second launch joins them (in the workgroup that comes last it took longer:
+// 11 rows of 8 sequences over 3000 slots 47 us, 39 so).
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_device.h"
 
 namespace sdsat {
 
 static constexpr float kRaise = 8.f;
+
+// parts of a tile's pages, where `tiles` of them (and key heads) leave compute units idle; tiles * Hkv * splits <= kPagedTileParts
+__device__ __forceinline__ int tile_splits(int tiles, int Hkv) {
+    return max(1, min(kPagedMaxTileParts, kPagedTileParts / max(1, tiles * Hkv)));
+}
 static constexpr int kWaves = 4;
+static constexpr int kTileSlices = 1;   // workgroups that join 32 rows of a tile, each some of the columns
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef unsigned long long u64;
 
 // acc += A(32 x 16) B(16 x 32): lane l holds A's row and B's column l % 32, contraction indices 8 (l / 32) .. + 7; of the
 // result column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4
@@ -97,13 +104,13 @@ struct Fetch {
 #pragma unroll
         for (int i = 0; i < VARS; ++i) off[i] = P::template source<RB>(i, lane) - i * 1024;
     }
-    template <int N, int I = 0>   // pieces first .. first + N - 1 (first a multiple of VARS), to their places
+    template <int N, int AUX, int I = 0>   // pieces first .. first + N - 1 (first a multiple of VARS), to their places
     __device__ __forceinline__ void pieces(const unsigned char* src, unsigned char* dst, int first) const {
         if constexpr (I < N) {
             const int at = (first + I / 4 * 4) * 1024;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_rsrc(src, P::HALF), (__attribute__((address_space(3))) void*)(dst + at), 16,
-                                                     off[I % VARS], at, I % 4 * 1024, 0);
-            pieces<N, I + 1>(src, dst, first);
+                                                     off[I % VARS], at, I % 4 * 1024, AUX);
+            pieces<N, AUX, I + 1>(src, dst, first);
         }
     }
 };
@@ -285,6 +292,7 @@ struct RowWave {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[n][i] = s[n][i];
         if (masked) {
+            asm volatile("" : "+v"(lane));   // nothing of the masks is formed ahead for the steps that need none
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -372,11 +380,9 @@ struct RowWave {
     }
 };
 
-template <typename V>
-__device__ __forceinline__ void agent_store(V* p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-template <typename V>
-__device__ __forceinline__ V agent_load(const V* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ u64 pack2(float lo, float hi) { return (u64)__float_as_uint(hi) << 32 | __float_as_uint(lo); }
+__device__ __forceinline__ void put4(__amdgpu_buffer_rsrc_t r, uint32_t off, f32x4_t v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), r, off, 0, 0);
+}
 
 // packed rows row0 .. row0 + rows - 1 of a chunk and key head
 struct Rows { int b, h, row0, rows, group; PagedSeq seq; };
@@ -411,78 +417,53 @@ __device__ __forceinline__ Sight sight_of(const PagedAttnArgs& a, const Rows& r,
     return s;
 }
 
-// Parts 0 .. n - 1 of some rows joined by log-sum-exp in part order: part p's at part + p * stride, [row][DH + 4] with O
-// to the part's base, the base and the sum.
-template <typename T, int DH>
-__device__ void join_parts(const PagedAttnArgs& a, const Rows& r, const float* part, size_t stride, int n, float* smem) {
-    constexpr int D4 = DH / 4;
-    const int tid = threadIdx.x;
-    float2* s_w = reinterpret_cast<float2*>(smem);   // [part][row]
-    __syncthreads();
-    for (int i = tid; i < n * r.rows; i += 64 * kWaves) {
-        const u64 u = agent_load(reinterpret_cast<const u64*>(part + i / r.rows * stride + (size_t)(i % r.rows) * (DH + 4) + DH));
-        s_w[i] = float2{__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32))};
-    }
-    __syncthreads();
-    if (tid < r.rows) {
-        float top = -INFINITY, den = 0.f;
-        for (int p = 0; p < n; ++p) top = fmaxf(top, s_w[p * r.rows + tid].x);
-        for (int p = 0; p < n; ++p) {
-            float2& w = s_w[p * r.rows + tid];
-            w.x = w.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.x - top);
-            den = fmaf(w.x, w.y, den);
-        }
-        const float inv = den == 0.f ? 0.f : 1.0f / den;
-        for (int p = 0; p < n; ++p) s_w[p * r.rows + tid].x *= inv;
-    }
-    __syncthreads();
-    for (int e = tid; e < r.rows * D4; e += 64 * kWaves) {
-        const int i = e / D4, d = e % D4 * 4;
-        const float* src = part + (size_t)i * (DH + 4) + d;
-        f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int p0 = 0; p0 < n; p0 += 8) {
-            u64 u[8][2];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {   // past the last: the last again, not used
-                const u64* at = reinterpret_cast<const u64*>(src + (size_t)min(p0 + j, n - 1) * stride);
-                u[j][0] = agent_load(at);
-                u[j][1] = agent_load(at + 1);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (p0 + j < n) {
-                    const float w = s_w[(p0 + j) * r.rows + i].x;
-                    acc[0] = fmaf(w, __uint_as_float((uint32_t)u[j][0]), acc[0]);
-                    acc[1] = fmaf(w, __uint_as_float((uint32_t)(u[j][0] >> 32)), acc[1]);
-                    acc[2] = fmaf(w, __uint_as_float((uint32_t)u[j][1]), acc[2]);
-                    acc[3] = fmaf(w, __uint_as_float((uint32_t)(u[j][1] >> 32)), acc[3]);
-                }
-        }
-        store_row<T, DH>(a, r, i, d, acc);
-    }
-}
-
+// A part of R rows (32 at most): [DH / 4][R] quads of O to the part's base, whole lines as the waves hold them, then [R]
+// quads of the base and the sum.
 template <int DH>
-__device__ __forceinline__ void store_part(float* part, int i, int d, f32x4_t v) {
-    u64* at = reinterpret_cast<u64*>(part + (size_t)i * (DH + 4) + d);
-    agent_store(at, pack2(v[0], v[1]));
-    agent_store(at + 1, pack2(v[2], v[3]));
-}
+constexpr int kPartFloats = 32 * (DH + 4);
+template <int DH>
+__device__ __forceinline__ uint32_t part_quad(int R, int i, int d4) { return (uint32_t)(d4 * R + i) * 16; }   // d4 = DH / 4: base, sum
 
-// This workgroup's part is stored; true for the last of n, which finds all of them.  The count is left at zero.
-__device__ __forceinline__ bool arrive(int* counter, int n) {
-    __shared__ int s_last;
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0);   // the stores, which write through, are at their place
-    asm volatile("" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const int old = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = old == n - 1;
-        if (s_last) agent_store(counter, 0);
+// LDS: pages, the waves' bases and sums.
+template <typename T, int DH>
+constexpr int kLdsBytes = kWaves * PageTile<T, DH>::BLK + 2 * kWaves * 32 * 4;
+
+// A call's work in pieces, numbered through the sequences: where piece `want` is, and how many there are.  pieces(lane's
+// sequence) counts those of one; 64 sequences are looked at at once.
+struct Found { bool ok; int b, k; PagedSeq seq; };
+template <typename F>
+__device__ __forceinline__ Found find_piece(const PagedSeqs& s, int want, int lane, F pieces) {
+    for (int b0 = 0; b0 < s.B; b0 += 64) {
+        const int b = b0 + lane;
+        PagedSeq q = load_seq(s, min(b, s.B - 1));
+        const int mine = b < s.B ? pieces(q) : 0;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += v;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        if (want < all) {
+            const int at = __popcll(__ballot(upto <= want));   // the first lane whose sum passes it
+            const int k = want - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
+            return Found{true, b0 + at, k, PagedSeq{__builtin_amdgcn_readlane(q.start, at), __builtin_amdgcn_readlane(q.n, at),
+                                                    __builtin_amdgcn_readlane(q.len, at), true}};
+        }
+        want -= all;
     }
-    __syncthreads();
-    return s_last;
+    return Found{false, 0, 0, PagedSeq{0, 0, 0, false}};
+}
+template <typename F>
+__device__ __forceinline__ int count_pieces(const PagedSeqs& s, int lane, F pieces) {
+    int all = 0;
+    for (int b0 = 0; b0 < s.B; b0 += 64) {
+        const int b = b0 + lane;
+        all = min(all + (b < s.B ? pieces(load_seq(s, b)) : 0), 1 << 24);   // starts that do not ascend: no overflow either
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o, 64);
+    return __builtin_amdgcn_readfirstlane(all);
 }
 
 // Pages lo .. hi - 1 that packed rows row0 .. see between them.
@@ -494,6 +475,12 @@ __device__ __forceinline__ void page_range(const PagedAttnArgs& a, const Rows& r
 }
 
 // ------------------------------------------------------------------ short chunks
+// Where a part of rows row0 .. of a short chunk goes.
+template <int DH>
+__device__ __forceinline__ float* few_part(const PagedAttnArgs& a, const Rows& r, int part) {
+    return a.part + ((((size_t)r.b * a.Hkv + r.h) * a.max_parts + part) * (kPagedFewRows / 32) + r.row0 / 32) * kPartFloats<DH>;
+}
+
 // Rows (at most 32) over pages lo .. hi - 1 of part sp (of `parts`, the first being part sp0).
 template <typename T, int DH>
 __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, int lo, int hi, int sp, int sp0, int parts,
@@ -526,8 +513,8 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
         w.load_q(q_row<T, DH>(a, r, lane & 31), lane);
         __builtin_amdgcn_sched_barrier(0);
         int id = __builtin_amdgcn_readlane(ids, 0);
-        fk.template pieces<P::PIECES>(kb + (size_t)id * page_bytes, s_k, 0);
-        fv.template pieces<P::PIECES>(vb + (size_t)id * page_bytes, s_v, 0);
+        fk.template pieces<P::PIECES, 2>(kb + (size_t)id * page_bytes, s_k, 0);
+        fv.template pieces<P::PIECES, 2>(vb + (size_t)id * page_bytes, s_v, 0);
         w.have_q();
         const PageRead<T, DH> rd(smem, wave * P::BLK, lane);
         for (int i = 0; i < cnt; ++i) {
@@ -542,7 +529,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
             if (more) {
                 if (((i + 1) & 63) == 0) load_ids(i + 1);
                 id = __builtin_amdgcn_readlane(ids, (i + 1) & 63);
-                fk.template pieces<P::PIECES>(kb + (size_t)id * page_bytes, s_k, 0);
+                fk.template pieces<P::PIECES, 2>(kb + (size_t)id * page_bytes, s_k, 0);
             }
             w.scores(s[0], f);
             w.weigh(s, p, blk, to, masked, see, a.scale, lane);
@@ -550,13 +537,13 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
             else wait_loads<0>();
             rd.template v<0>(f);
             if constexpr (sizeof(T) == 4) wait_lds();
-            if (more) fv.template pieces<P::PIECES>(vb + (size_t)id * page_bytes, s_v, 0);
+            if (more) fv.template pieces<P::PIECES, 2>(vb + (size_t)id * page_bytes, s_v, 0);
             w.weighted(p[0], f, masked);
         }
         if (bad) atomicOr(a.seq.err, 1);
     }
     // the waves' results, in their pieces of LDS, joined in wave order
-    __shared__ float s_base[kWaves][32], s_sum[kWaves][32];
+    float (*s_base)[32] = reinterpret_cast<float (*)[32]>(smem + kWaves * P::BLK), (*s_sum)[32] = s_base + kWaves;
     f32x4_t* own = reinterpret_cast<f32x4_t*>(smem + wave * P::BLK);
     static_assert(QUADS * 1024 <= P::BLK, "a wave's O fits its page");
     const float sum = w.whole_sum();
@@ -580,9 +567,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
         wt[k] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
         den = fmaf(wt[k], s_sum[k][i], den);
     }
-    const size_t stride = (size_t)kPagedFewRows * (DH + 4);
-    float* base = a.part + ((size_t)r.b * a.Hkv + r.h) * a.max_parts * stride + (size_t)r.row0 * (DH + 4);
-    float* mine = base + (sp - sp0) * stride;
+    const __amdgpu_buffer_rsrc_t rs = buf_rsrc(few_part<DH>(a, r, sp - sp0), kPartFloats<DH> * 4);
     const float inv = den == 0.f ? 0.f : 1.0f / den;
     for (int qd = wave; qd < QUADS; qd += kWaves) {
         f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -597,91 +582,80 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
         if (parts == 1) {
             store_row<T, DH>(a, r, i, d, acc * inv);
         } else {
-            store_part<DH>(mine, i, d, acc);
-            if (qd == 0 && lane < 32) agent_store(reinterpret_cast<u64*>(mine + (size_t)i * (DH + 4) + DH), pack2(top, den));
+            put4(rs, part_quad<DH>(r.rows, i, d / 4), acc);
+            if (qd == 0 && lane < 32) put4(rs, part_quad<DH>(r.rows, i, DH / 4), f32x4_t{top, den, 0.f, 0.f});
         }
     }
-    if (parts == 1) return;
-    int* counter = a.counter + ((size_t)r.b * a.Hkv + r.h) * (kPagedFewRows / 32) + r.row0 / 32;
-    if (arrive(counter, parts)) join_parts<T, DH>(a, r, base, stride, parts, reinterpret_cast<float*>(smem));
 }
 
 // Workgroup `wg` of `wgs` takes pieces wg, wg + wgs, ... of the short chunks': per sequence its parts, row tiles, key heads.
 template <typename T, int DH>
 __device__ __forceinline__ void few_work(const PagedAttnArgs& a, int wg, int wgs, unsigned char* smem, int wave, int lane) {
     const int group = a.H / a.Hkv;
+    auto whole = [&](const PagedSeq& q) { return Rows{0, 0, 0, q.n * group, group, q}; };
+    auto pieces = [&](const PagedSeq& q) {
+        if (q.n == 0 || q.n * (long)group > kPagedFewRows) return 0;
+        int lo, hi;
+        page_range(a, whole(q), lo, hi);
+        return ((hi - 1) / a.per_split - lo / a.per_split + 1) * ((q.n * group + 31) / 32) * a.Hkv;
+    };
     for (int want = wg;; want += wgs) {
-        int before = 0;
-        Rows r;
-        int lo = 0, hi = 0, sp = 0, sp0 = 0, parts = 0;
-        bool found = false;
-        for (int b0 = 0; b0 < a.seq.B && !found; b0 += 64) {
-            // 64 sequences at a time: their pieces, and the sums up to each
-            const int b = b0 + lane, bc = min(b, a.seq.B - 1);
-            const PagedSeq q = load_seq(a.seq, bc);
-            Rows x{bc, 0, 0, q.n * group, group, q};
-            int l = 0, u = 0, mine = 0, tiles = 0, first = 0;
-            if (b < a.seq.B && q.n > 0 && q.n * (long)group <= kPagedFewRows) {
-                page_range(a, x, l, u);
-                first = l / a.per_split;
-                mine = (u - 1) / a.per_split - first + 1;
-                tiles = (x.rows + 31) / 32;
-            }
-            const int pieces = mine * tiles * a.Hkv;
-            int upto = pieces;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int v = __shfl_up(upto, o, 64);
-                if (lane >= o) upto += v;
-            }
-            const int all = __builtin_amdgcn_readlane(upto, 63);
-            if (want < before + all) {
-                const int at = __popcll(__ballot(before + upto <= want));   // the first lane whose sum passes it
-                const int k = want - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(pieces, at));
-                found = true;
-                r.b = b0 + at;
-                r.group = group;
-                r.seq = PagedSeq{__builtin_amdgcn_readlane(q.start, at), __builtin_amdgcn_readlane(q.n, at),
-                                 __builtin_amdgcn_readlane(q.len, at), true};
-                lo = __builtin_amdgcn_readlane(l, at);
-                hi = __builtin_amdgcn_readlane(u, at);
-                sp0 = __builtin_amdgcn_readlane(first, at);
-                parts = __builtin_amdgcn_readlane(mine, at);
-                const int t = __builtin_amdgcn_readlane(tiles, at);
-                r.h = k % a.Hkv;
-                r.row0 = k / a.Hkv % t * 32;
-                r.rows = min(32, r.seq.n * group - r.row0);
-                sp = sp0 + k / a.Hkv / t;
-            }
-            before += all;
-        }
-        if (!found) return;
-        few_rows<T, DH>(a, r, lo, hi, sp, sp0, parts, smem, wave, lane);
+        const Found f = find_piece(a.seq, want, lane, pieces);
+        if (!f.ok) return;
+        Rows r = whole(f.seq);
+        int lo, hi;
+        page_range(a, r, lo, hi);
+        const int sp0 = lo / a.per_split, parts = (hi - 1) / a.per_split - sp0 + 1, tiles = (r.rows + 31) / 32;
+        r.b = f.b;
+        r.h = f.k % a.Hkv;
+        r.row0 = f.k / a.Hkv % tiles * 32;
+        r.rows = min(32, r.rows - r.row0);
+        few_rows<T, DH>(a, r, lo, hi, sp0 + f.k / a.Hkv / tiles, sp0, parts, smem, wave, lane);
         __syncthreads();   // smem is free
     }
 }
 
 // ------------------------------------------------------------------ tiles
+// Where rows 32 sub .. of a tile's part go.
+template <int DH>
+__device__ __forceinline__ float* tile_part(const PagedAttnArgs& a, int part, int sub) {
+    return a.part + a.tile_part + ((size_t)part * (kPagedTileRows / 32) + sub) * kPartFloats<DH>;
+}
+
+// Piece `want` of the tiles: a tile and key head (numbered `slot` among them) and one of its parts, pages lo .. hi - 1 of it.
+struct TileWork { bool ok; Rows r; int slot, splits, sp, parts, lo, hi; };
+__device__ __forceinline__ TileWork tile_work(const PagedAttnArgs& a, int want, bool by_slot, int lane) {
+    const int group = a.H / a.Hkv;
+    auto tiles_of = [&](const PagedSeq& q) {
+        return q.n * (long)group > kPagedFewRows ? (q.n * group + kPagedTileRows - 1) / kPagedTileRows : 0;
+    };
+    TileWork t{};
+    t.splits = tile_splits(count_pieces(a.seq, lane, tiles_of), a.Hkv);
+    const int each = by_slot ? 1 : t.splits;
+    const Found f = find_piece(a.seq, want, lane, [&](const PagedSeq& q) { return tiles_of(q) * each * a.Hkv; });
+    if (!f.ok) return t;
+    const int h = f.k % a.Hkv, nth = f.k / a.Hkv / each;
+    t.sp = f.k / a.Hkv % each;
+    t.slot = (want - f.k) / each + nth * a.Hkv + h;
+    t.r = Rows{f.b, h, (tiles_of(f.seq) - 1 - nth) * kPagedTileRows, 0, group, f.seq};   // the longest first
+    t.r.rows = min(kPagedTileRows, f.seq.n * group - t.r.row0);
+    page_range(a, t.r, t.lo, t.hi);
+    const int per = max((t.hi - t.lo + t.splits - 1) / t.splits, 4);
+    t.parts = (t.hi - t.lo + per - 1) / per;
+    t.ok = t.sp < t.parts;
+    t.lo += t.sp * per;
+    t.hi = min(t.hi, t.lo + per);
+    return t;
+}
+
 template <typename T, int DH>
 __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsigned char* smem, int wave, int lane) {
     using P = PageTile<T, DH>;
-    constexpr int DT = DH / 32, NL = P::PIECES / 2;   // 1 KiB loads of a wave per step and operand
-    const int group = a.H / a.Hkv;
-    const int h = wg % a.Hkv, sp = wg / a.Hkv % a.splits, piece = wg / a.Hkv / a.splits;
-    const int b = __builtin_amdgcn_readfirstlane(seq_of_piece(a.seq, piece, group, kPagedTileRows, 1, lane));
-    Rows r{b, h, 0, 0, group, load_seq(a.seq, b)};
-    if (!r.seq.ok || r.seq.n * (long)group <= kPagedFewRows) return;
-    const int packed = r.seq.n * group, tiles = (packed + kPagedTileRows - 1) / kPagedTileRows;
-    const int nth = piece - piece_begin(r.seq.start, group, kPagedTileRows, 1, b);
-    if (nth < 0 || nth >= tiles) return;
-    r.row0 = (tiles - 1 - nth) * kPagedTileRows;   // the longest first
-    r.rows = min(kPagedTileRows, packed - r.row0);
-    int lo, hi;
-    page_range(a, r, lo, hi);
-    const int per = (hi - lo + a.splits - 1) / a.splits, parts = (hi - lo + per - 1) / per;
-    if (sp >= parts) return;
-    lo += sp * per;
-    hi = min(hi, lo + per);
+    constexpr int DT = DH / 32, NL = P::PIECES / 2;   // 1 KiB loads of a wave per step, of K and of V
+    const TileWork t = tile_work(a, wg, false, lane);
+    if (!t.ok) return;
+    const Rows r = t.r;
+    const int b = r.b, h = r.h, lo = t.lo, hi = t.hi, parts = t.parts;
     const int w0 = 32 * wave;
     const Sight see = sight_of<T, DH>(a, r, w0, lane);
     // pages this wave's rows see
@@ -714,8 +688,8 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
         const int j = min(2 * i + (wave >> 1), hi - lo - 1);
         const size_t off = (size_t)__builtin_amdgcn_readlane(ids, j & 63) * page_bytes;
         unsigned char* dst = smem + (i & 1) * 2 * P::BLK + (wave >> 1) * P::BLK;
-        fk.template pieces<NL>(kb + off, dst, part0);
-        fv.template pieces<NL>(vb + off, dst + P::HALF, part0);
+        fk.template pieces<NL, 0>(kb + off, dst, part0);
+        fv.template pieces<NL, 0>(vb + off, dst + P::HALF, part0);
     };
     w.load_q(q_row<T, DH>(a, r, w0 + (lane & 31)), lane);
     __builtin_amdgcn_sched_barrier(0);
@@ -748,81 +722,167 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
     }
     if (bad) atomicOr(a.seq.err, 1);
     const float den = w.whole_sum(), inv = den == 0.f ? 0.f : 1.0f / den;
-    const size_t stride = (size_t)kPagedTileRows * (DH + 4);
-    float* base = a.part + a.tile_part + ((size_t)piece * a.Hkv + h) * a.splits * stride;
-    float* mine = base + sp * stride;
-    const int i = w0 + (lane & 31);
-    if (i < r.rows) {
+    const __amdgpu_buffer_rsrc_t rs = buf_rsrc(tile_part<DH>(a, t.slot * t.splits + t.sp, wave), kPartFloats<DH> * 4);
+    const int own = min(32, r.rows - w0), i = lane & 31;   // rows of this wave
+    if (i >= own) return;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f32x4_t v = f32x4_t{w.o[dt][4 * j], w.o[dt][4 * j + 1], w.o[dt][4 * j + 2], w.o[dt][4 * j + 3]};
-                const int d = 32 * dt + 8 * j + 4 * (lane >> 5);
-                if (parts == 1) store_row<T, DH>(a, r, i, d, v * inv);
-                else store_part<DH>(mine, i, d, v);
-            }
-        if (parts > 1 && lane < 32) agent_store(reinterpret_cast<u64*>(mine + (size_t)i * (DH + 4) + DH), pack2(w.base, den));
-    }
-    if (parts == 1) return;
-    int* counter = a.counter + (size_t)a.seq.B * a.Hkv * (kPagedFewRows / 32) + (size_t)piece * a.Hkv + h;
-    if (arrive(counter, parts)) join_parts<T, DH>(a, r, base, stride, parts, reinterpret_cast<float*>(smem));
+        for (int j = 0; j < 4; ++j) {
+            const f32x4_t v = f32x4_t{w.o[dt][4 * j], w.o[dt][4 * j + 1], w.o[dt][4 * j + 2], w.o[dt][4 * j + 3]};
+            const int d = 32 * dt + 8 * j + 4 * (lane >> 5);
+            if (parts == 1) store_row<T, DH>(a, r, w0 + i, d, v * inv);
+            else put4(rs, part_quad<DH>(own, i, d / 4), v);
+        }
+    if (parts > 1 && lane < 32) put4(rs, part_quad<DH>(own, i, DH / 4), f32x4_t{w.base, den, 0.f, 0.f});
 }
 
+// ------------------------------------------------------------------ joining parts
+// Parts 0 .. n - 1 of rows (at most 32) joined by log-sum-exp, part p's at part + p * stride quads; columns
+// of slice `slice` of `slices`.  Even parts in order, odd ones in order, then both: half a wave each.
+template <typename T, int DH>
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Rows& r, const f32x4_t* part, int stride, int n, int slice,
+                                           int slices, float (*s_w)[32]) {
+    constexpr int D4 = DH / 4;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    static_assert(kPagedMaxParts <= 64, "a lane for each part");
+    // a row's bases and sums in the lanes of a wave; the waves take the rows in turn
+    for (int i = tid / 64; i < r.rows; i += 4) {
+        const f32x4_t v = part[(size_t)min(lane, n - 1) * stride + D4 * r.rows + i];
+        const float m = lane < n ? v[0] : -INFINITY, top = across_wave(m, OpMax());
+        const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        const float den = across_wave(lane < n ? w * v[1] : 0.f, OpSum());
+        if (lane < n) s_w[lane][i] = w * (den == 0.f ? 0.f : 1.0f / den);
+    }
+    __syncthreads();
+    const int quads = r.rows * (D4 / slices);
+    const int e0 = tid / 64 * 32 + (lane & 31);
+    auto join = [&](auto ahead) {   // so many parts' loads of a half wave under way at once, of 16 / AHEAD quads
+        constexpr int AHEAD = decltype(ahead)::value, Q = 16 / AHEAD > 8 ? 8 : 16 / AHEAD;
+        for (int eb = e0; eb - e0 < quads; eb += 128 * Q) {
+            f32x4_t acc[Q];
+#pragma unroll
+            for (int k = 0; k < Q; ++k) acc[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int p0 = half; p0 < n; p0 += 2 * AHEAD) {
+                f32x4_t u[Q][AHEAD];
+#pragma unroll
+                for (int k = 0; k < Q; ++k)
+#pragma unroll
+                    for (int j = 0; j < AHEAD; ++j)   // past the last: the last again, not used
+                        u[k][j] = part[(size_t)min(p0 + 2 * j, n - 1) * stride + slice * (D4 / slices) * r.rows + min(eb + 128 * k, quads - 1)];
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int k = 0; k < Q; ++k)
+#pragma unroll
+                    for (int j = 0; j < AHEAD; ++j) {
+                        const bool in = p0 + 2 * j < n;
+                        const float w = s_w[min(p0 + 2 * j, n - 1)][min(eb + 128 * k, quads - 1) % r.rows];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[k][c] = in ? fmaf(w, u[k][j][c], acc[k][c]) : acc[k][c];
+                    }
+            }
+#pragma unroll
+            for (int k = 0; k < Q; ++k) {
+                const int e = eb + 128 * k;
+                f32x4_t out;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) out[c] = acc[k][c] + __shfl_xor(acc[k][c], 32, 64);
+                if (half == 0 && e < quads) store_row<T, DH>(a, r, e % r.rows, 4 * (slice * (D4 / slices) + e / r.rows), out);
+            }
+        }
+    };
+    if (n <= 2) join(std::integral_constant<int, 1>());
+    else if (n <= 8) join(std::integral_constant<int, 4>());
+    else join(std::integral_constant<int, 16>());
+}
+
+// Workgroups of short chunks, `slices` for each sequence, key head and one of `subs` times 32 rows; then of tiles, four for
+// each 32 rows of one.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a, int few, int subs, int slices) {
+    __shared__ float s_w[kPagedMaxParts][32];
+    const int lane = threadIdx.x & 63;
+    int x = (int)blockIdx.x;
+    const int group = a.H / a.Hkv;
+    if (x < few) {
+        const int slice = x % slices;
+        x /= slices;
+        Rows r{0, 0, x % subs * 32, 0, group, {}};
+        x /= subs;
+        r.h = x % a.Hkv;
+        r.b = x / a.Hkv;
+        r.seq = load_seq(a.seq, r.b);
+        const int rows = r.seq.n * group;
+        if (rows <= r.row0 || rows > kPagedFewRows) return;
+        int lo, hi;
+        page_range(a, Rows{r.b, 0, 0, rows, group, r.seq}, lo, hi);
+        const int parts = (hi - 1) / a.per_split - lo / a.per_split + 1;
+        if (parts < 2) return;
+        r.rows = min(32, rows - r.row0);
+        join_parts<T, DH>(a, r, reinterpret_cast<const f32x4_t*>(few_part<DH>(a, r, 0)), kPagedFewRows / 32 * kPartFloats<DH> / 4, parts,
+                          slice, slices, s_w);
+        return;
+    }
+    x -= few;
+    const int slice = x % kTileSlices, sub = x / kTileSlices % (kPagedTileRows / 32);
+    const TileWork t = tile_work(a, x / kTileSlices / (kPagedTileRows / 32), true, lane);
+    if (!t.ok || t.parts < 2 || 32 * sub >= t.r.rows) return;
+    Rows r = t.r;
+    r.row0 += 32 * sub;
+    r.rows = min(32, r.rows - 32 * sub);
+    join_parts<T, DH>(a, r, reinterpret_cast<const f32x4_t*>(tile_part<DH>(a, t.slot * t.splits, sub)),
+                      kPagedTileRows / 32 * kPartFloats<DH> / 4, t.parts, slice, kTileSlices, s_w);
+}
+
+// ------------------------------------------------------------------ the launch
 template <typename T, int DH, bool TILES>
 __global__ void __launch_bounds__(64 * kWaves, sizeof(T) * DH > 256 ? 1 : 2) paged_attn_kernel(PagedAttnArgs a) {
-    __shared__ __align__(1024) unsigned char smem[kWaves * PageTile<T, DH>::BLK];
+    __shared__ __align__(1024) unsigned char smem[kLdsBytes<T, DH>];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (blockIdx.x == 0 && wave == 0) check_seqs(a.seq, lane);
+    int few = (int)blockIdx.x;
     if constexpr (TILES) {
-        if ((int)blockIdx.x < a.tile_wgs) {
-            tile_rows<T, DH>(a, (int)blockIdx.x, smem, wave, lane);
+        if (few < a.tile_wgs) {
+            tile_rows<T, DH>(a, few, smem, wave, lane);
             return;
         }
+        few -= a.tile_wgs;
     }
-    few_work<T, DH>(a, (int)blockIdx.x - a.tile_wgs, (int)gridDim.x - a.tile_wgs, smem, wave, lane);
+    few_work<T, DH>(a, few, a.few_wgs, smem, wave, lane);
 }
 
 // ------------------------------------------------------------------ plans
 PagedPlan plan_paged(int Hkv, int max_batch, int max_ctx) {
     PagedPlan p{};
     const long cap = std::max(1, (max_ctx + kPage - 1) / kPage), pairs = (long)Hkv * max_batch;
-    // pages of a part: a full cache in about 1024 parts, four for each wave at the least
-    long per = std::max<long>(4, std::min<long>((cap * pairs + 1023) / 1024, 64));
+    // pages of a part: a full cache in about 1024 parts, four for each wave at the least.  us with 4, 8 and 16 at the least: a
+    // token over 1500 slots of 8 key heads 15.1, 14.1, 15.1; 6 tokens of 4 sequences over 3000 37, 26, 20; 64 tokens over 500
+    // slots 39, 39, 26; 11 rows of 4 sequences over 1500 slots of 32 heads 33, 31, 28.  512 to 4096 parts, 64 tokens over 4000
+    // slots: 167, 167, 173, 181.
+    long per = std::max<long>(16, std::min<long>((cap * pairs + 1023) / 1024, 64));
     per = std::max(per, (cap + kPagedMaxParts - 1) / kPagedMaxParts);
     p.per_split = (int)per;
     p.max_parts = (int)((cap + per - 1) / per);
     return p;
 }
 
-static long tile_pieces(int H, int Hkv, long rows, int B) { return rows * (H / Hkv) / kPagedTileRows + B; }
-
-// parts of a tile's pages: as many as fill the compute units twice
-static int tile_splits(long pieces, int Hkv) { return (int)std::max<long>(1, std::min<long>(kPagedMaxTileParts, 512 / (pieces * Hkv))); }
+// tiles of a call and key head, at most
+static long most_tiles(int H, int Hkv, long rows, int B) { return rows * (H / Hkv) / kPagedTileRows + B; }
 
 void plan_paged_call(PagedPlan& p, int H, int Hkv, int B, int rows, int max_q, int max_len) {
     const int group = H / Hkv;
-    p.splits = 1;
     p.tile_wgs = 0;
-    if ((long)max_q * group > kPagedFewRows) {
-        const long pieces = tile_pieces(H, Hkv, rows, B);
-        p.splits = std::min(tile_splits(pieces, Hkv), (max_len + 4 * kPage - 1) / (4 * kPage));
-        p.tile_wgs = (int)std::min<long>(pieces * Hkv * p.splits, 0x7FFFFFFF);
-    }
+    if ((long)max_q * group > kPagedFewRows)
+        p.tile_wgs = (int)std::min<long>(std::max<long>(most_tiles(H, Hkv, rows, B) * Hkv, kPagedTileParts), 0x7FFFFFFF);
     const int tiles = (int)std::min<long>(((long)max_q * group + 31) / 32, kPagedFewRows / 32);
     const long parts = ((long)max_len + kPage * p.per_split - 1) / (kPage * p.per_split);
+    p.call_parts = (int)parts;
     p.few_wgs = (int)std::max<long>(1, std::min<long>(parts * B * tiles * Hkv, 2048));
 }
 
 size_t paged_part_floats(const PagedPlan& p, int H, int Hkv, int head_dim, int max_batch, int max_rows, size_t* tile_part) {
-    const size_t few = p.max_parts > 1 ? (size_t)max_batch * Hkv * p.max_parts * kPagedFewRows * (head_dim + 4) : 0;
-    // pieces * Hkv * splits <= 512 wherever splits > 1; where there are fewer pieces, splits are bounded
-    *tile_part = few;
-    return few + ((long)max_rows * (H / Hkv) > kPagedFewRows ? (size_t)512 * kPagedTileRows * (head_dim + 4) : 0);
-}
-
-size_t paged_counter_ints(int H, int Hkv, int max_batch, int max_rows) {
-    return (size_t)max_batch * Hkv * (kPagedFewRows / 32) + (size_t)tile_pieces(H, Hkv, max_rows, max_batch) * Hkv;
+    *tile_part = p.max_parts > 1 ? (size_t)max_batch * Hkv * p.max_parts * kPagedFewRows * (head_dim + 4) : 0;
+    return *tile_part + ((long)max_rows * (H / Hkv) > kPagedFewRows ? (size_t)kPagedTileParts * kPagedTileRows * (head_dim + 4) : 0);
 }
 
 template <typename T, int DH>
@@ -832,6 +892,11 @@ static hipError_t launch_dh(const PagedPlan& p, const PagedAttnArgs& a, hipStrea
         hipLaunchKernelGGL((paged_attn_kernel<T, DH, true>), dim3(grid), dim3(64 * kWaves), 0, s, a);
     else
         hipLaunchKernelGGL((paged_attn_kernel<T, DH, false>), dim3(grid), dim3(64 * kWaves), 0, s, a);
+    // tiles in several parts are kPagedTileParts / 2 at the most, with key heads
+    const int subs = (long)a.seq.max_q * (a.H / a.Hkv) > 32 ? kPagedFewRows / 32 : 1, slices = p.call_parts > 8 ? 4 : 1;
+    const int few = p.call_parts > 1 ? a.seq.B * a.Hkv * subs * slices : 0;
+    const int join = few + (p.tile_wgs ? kPagedTileParts / 2 * (kPagedTileRows / 32) * kTileSlices : 0);
+    if (join) hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3((unsigned)join), dim3(256), 0, s, a, few, subs, slices);
     return hipGetLastError();
 }
 
@@ -841,13 +906,12 @@ hipError_t launch_paged_attention(int dtype, int head_dim, const PagedPlan& p, c
     if (group < 1 || a.H % a.Hkv || q.B < 1 || q.rows < 0 || q.pages_ld < 1 || q.n_pages < 1 || q.max_q < 0 || q.max_len < 0 ||
         q.max_len > (long)q.pages_ld * kPage || !q.start || !q.len || !q.pages || !q.err || !a.kp || !a.vp || !a.q || !a.out ||
         (a.mask && (q.max_q > 64 || a.window)) || a.window < 0 || !(a.scale > 0.f) || a.ldq % 8 || a.ldo % 4 || p.per_split < 1 ||
-        a.per_split != p.per_split || a.splits != p.splits || a.tile_wgs != p.tile_wgs || a.max_parts != p.max_parts ||
-        p.splits < 1 || p.splits > kPagedMaxTileParts || p.few_wgs < 1 || p.max_parts > kPagedMaxParts ||
-        (long)p.tile_wgs + p.few_wgs > 0x7FFFFFFFl / (64 * kWaves) || q.max_len > (long)p.max_parts * p.per_split * kPage ||
-        (long)p.max_parts * p.per_split > 0x7FFFFFFFl / kPage || !a.part || !a.counter ||
-        (p.tile_wgs && p.tile_wgs != tile_pieces(a.H, a.Hkv, q.rows, q.B) * a.Hkv * p.splits) ||
-        ((long)q.max_q * group > kPagedFewRows && !p.tile_wgs) ||
-        (p.splits > 1 && tile_pieces(a.H, a.Hkv, q.rows, q.B) * a.Hkv * p.splits > 512))
+        a.per_split != p.per_split || a.tile_wgs != p.tile_wgs || a.few_wgs != p.few_wgs || a.max_parts != p.max_parts ||
+        p.few_wgs < 1 || p.max_parts > kPagedMaxParts ||
+        (long)p.tile_wgs + p.few_wgs > 0x7FFFFFFFl / (64 * kWaves) || q.max_len > (long)p.max_parts * p.per_split * kPage || p.call_parts < 1 ||
+        (long)p.call_parts * p.per_split * kPage < q.max_len || (long)q.B * a.Hkv > 0x7FFFFFFFl / 4096 ||
+        (long)p.max_parts * p.per_split > 0x7FFFFFFFl / kPage || !a.part ||
+        ((long)q.max_q * group > kPagedFewRows && p.tile_wgs < std::max<long>(most_tiles(a.H, a.Hkv, q.rows, q.B) * a.Hkv, kPagedTileParts)))
         return hipErrorInvalidValue;
     if (dtype == 1) {
         if (head_dim == 128) return launch_dh<uint16_t, 128>(p, a, s);
