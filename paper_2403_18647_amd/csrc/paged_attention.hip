@@ -8,7 +8,7 @@
 //
 // The scores of 32 slots and 32 packed rows are formed as S^T = K Q^T, so that a lane has 16 slots of one row (its row's
 // others are in lane ^ 32), and enter O^T += V^T P^T as they stand: K's rows are read in the order in which V's pages hold
-// their slots.  P is rounded to the cache's type (half a step of bf16, 2^-9 of each weight, on the way to an output that
+// their slots.  P is rounded to the cache's type (half a step of bf16, 2^-8 of each weight at the most, on the way to an output that
 // is rounded as coarsely; the row's sum takes the unrounded weights); scores, sums and O are float.  A row keeps a base,
 // in units of log 2, that its weights are 2 to the score above; the base is raised, and O scaled, only when a score passes
 // it by more than kRaise: in most blocks nothing is scaled.
