@@ -41,16 +41,22 @@ __device__ __forceinline__ void check_seqs(const PagedSeqs& s, int lane) {
 __device__ __forceinline__ int piece_begin(int start, int mul, int unit, int extra, int b) {
     return (int)((long)start * mul / unit) + extra * b;
 }
-__device__ __forceinline__ int seq_of_piece(const PagedSeqs& s, int piece, int mul, int unit, int extra, int lane) {
-    int before = 0;
-    for (int b0 = 0; b0 < s.B; b0 += 64) {
-        const int b = b0 + lane;
-        const unsigned long long in =
-            __ballot(b < s.B && piece_begin(s.start[min(b, s.B - 1)], mul, unit, extra, b) <= piece);
+struct PieceSeq { int b; PagedSeq seq; };
+__device__ __forceinline__ PieceSeq seq_of_piece(const PagedSeqs& s, int piece, int mul, int unit, int extra, int lane) {
+    int before = 0, b0 = 0, start, end, len;   // this lane's sequence's
+    for (;; b0 += 64) {
+        const int b = b0 + lane, bc = min(b, s.B - 1);
+        start = s.start[bc];
+        end = s.start[bc + 1];
+        len = s.len[bc];
+        const unsigned long long in = __ballot(b < s.B && piece_begin(start, mul, unit, extra, b) <= piece);
         before += __popcll(in);
-        if (in != ~0ull) break;
+        if (in != ~0ull || b0 + 64 >= s.B) break;
     }
-    return max(before, 1) - 1;
+    const int b = max(before, 1) - 1;
+    if (b < b0) return {b, load_seq(s, b)};   // the last of the 64 before
+    const int l = b - b0;
+    return {b, check_seq(s, __builtin_amdgcn_readlane(start, l), __builtin_amdgcn_readlane(end, l), __builtin_amdgcn_readlane(len, l))};
 }
 
 }  // namespace sdsat
