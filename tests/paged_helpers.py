@@ -136,7 +136,7 @@ def assert_within(got, want, tol, what=""):
     bad = ~(off <= tol)
     assert not bad.any(), (f"{what}: {int(bad.sum())} of {bad.numel()} off, first at {bad.nonzero()[0].tolist()}, "
                            f"worst {float((off / tol).nan_to_num(math.inf).max()):.3g} of what is allowed")
-    return float((off / tol).max())
+    return float((off / tol).max()) if off.numel() else 0.0
 
 
 def tree_mask(n, width=2):
