@@ -321,11 +321,11 @@ int sdsat_generate_forced(sdsat_ctx* ctx, int32_t batch, const int32_t* h_prompt
 typedef struct sdsat_paged sdsat_paged;   /* opaque, library-owned handle */
 
 typedef struct sdsat_paged_config {
-    int32_t n_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
+    int32_t n_heads, n_kv_heads, head_dim;   /* n_heads at most 1024, head_dim 64 or 128 */
     int32_t dtype;                           /* of the pool, queries and (or float) outputs */
     int32_t n_pages;                         /* pages of each pool */
-    int32_t max_rows;                        /* new tokens of a call, of all its sequences */
-    int32_t max_batch;                       /* sequences of a call */
+    int32_t max_rows;                        /* new tokens of a call, of all its sequences: at most 2^20 */
+    int32_t max_batch;                       /* sequences of a call: at most 4096, times n_kv_heads 2^19 */
     int32_t max_ctx;                         /* slots of a sequence, at most 2^24 */
 } sdsat_paged_config;
 

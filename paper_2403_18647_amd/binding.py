@@ -506,7 +506,8 @@ class Paged:
         self.cfg = cfg
         self.workspace = torch.empty(sdsat_paged_query_sizes(cfg), dtype=torch.uint8, device=device)
         self.stream = torch.cuda.current_stream(device)
-        self.handle = sdsat_paged_init(cfg, self.workspace, self.stream)
+        with torch.cuda.device(self.workspace.device):   # the handle's device is the one that is current here
+            self.handle = sdsat_paged_init(cfg, self.workspace, self.stream)
 
     def pool(self):
         """K [pages, kv_heads, 32, head_dim] and V [pages, kv_heads, head_dim, 32], uninitialised."""

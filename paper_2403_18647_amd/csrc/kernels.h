@@ -217,6 +217,7 @@ hipError_t launch_paged_append(int dtype, int x_dtype, int head_dim, const Paged
 // kPagedFewRows packed rows are cut into parts of per_split pages, counted from slot 0, longer ones into tiles of
 // kPagedTileRows packed rows, and each tile's pages into parts where there are few tiles.
 constexpr int kPagedFewRows = 64, kPagedTileRows = 128;
+constexpr int kPagedMaxPairs = 1 << 19;  // sequences and key heads of a call (a launch's 2^32 threads)
 constexpr int kPagedMaxParts = 64;       // parts of a short chunk, at most
 constexpr int kPagedMaxTileParts = 16;   // parts of a tile, at most
 constexpr int kPagedTileParts = 512;    // of all tiles and key heads, at most, where tiles have several

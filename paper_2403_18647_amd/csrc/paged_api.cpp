@@ -55,8 +55,9 @@ int check_config(const sdsat_paged_config* c, std::string* why) {
     if (c->n_heads % c->n_kv_heads) { *why = "n_heads must be a multiple of n_kv_heads"; return SDSAT_EINVAL; }
     if (c->dtype != SDSAT_DTYPE_FP32 && c->dtype != SDSAT_DTYPE_BF16) { *why = "dtype must be 0 or 1"; return SDSAT_EINVAL; }
     if (c->head_dim != 64 && c->head_dim != 128) { *why = "head_dim must be 64 or 128"; return SDSAT_EUNSUPPORTED; }
-    if (c->n_heads > kMaxHeads || c->max_batch > kMaxPagedBatch || c->max_rows > kMaxPagedRows || c->max_ctx > kMaxPagedCtx) {
-        *why = "n_heads <= 1024, max_batch <= 4096, max_rows <= 2^20 and max_ctx <= 2^24 are supported";
+    if (c->n_heads > kMaxHeads || c->max_batch > kMaxPagedBatch || c->max_rows > kMaxPagedRows || c->max_ctx > kMaxPagedCtx ||
+        (int64_t)c->max_batch * c->n_kv_heads > kPagedMaxPairs) {
+        *why = "n_heads <= 1024, max_batch <= 4096, max_batch * n_kv_heads <= 2^19, max_rows <= 2^20 and max_ctx <= 2^24 are supported";
         return SDSAT_EUNSUPPORTED;
     }
     return SDSAT_OK;

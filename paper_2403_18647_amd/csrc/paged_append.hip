@@ -263,9 +263,10 @@ static hipError_t launch_append_dh(int head_dim, const PagedAppendArgs& a, hipSt
     // in pairs
     int per = 20;
     while (per > 5 && (long)pieces * ((a.H + a.Hkv + per - 1) / per + (a.Hkv + per - 1) / per) < 1024) per /= 2;
-    const int pv = a.seq.max_q > kScatterTokens ? kTurned : per;
+    int pv = a.seq.max_q > kScatterTokens ? kTurned : per;
+    if ((long)pieces * (a.Hkv / pv) > 1 << 22) pv = std::max(pv, per);   // a launch's 2^32 threads
     const int slices = (a.H + a.Hkv + per - 1) / per + (a.Hkv + pv - 1) / pv;
-    if ((long)pieces * slices > 0x7FFFFFFFl / kAppendThreads) return hipErrorInvalidValue;
+    if ((long)pieces * slices > 0xFFFFFFFFl / kAppendThreads) return hipErrorInvalidValue;
     auto kern = head_dim == 128 ? paged_append_kernel<TX, T, 128> : paged_append_kernel<TX, T, 64>;
     hipLaunchKernelGGL(kern, dim3((unsigned)(pieces * slices)), dim3(kAppendThreads), 0, s, a, slices, per, pv);
     return hipGetLastError();

@@ -908,8 +908,8 @@ hipError_t launch_paged_attention(int dtype, int head_dim, const PagedPlan& p, c
         (a.mask && (q.max_q > 64 || a.window)) || a.window < 0 || !(a.scale > 0.f) || a.ldq % 8 || a.ldo % 4 || p.per_split < 1 ||
         a.per_split != p.per_split || a.tile_wgs != p.tile_wgs || a.few_wgs != p.few_wgs || a.max_parts != p.max_parts ||
         p.few_wgs < 1 || p.max_parts > kPagedMaxParts ||
-        (long)p.tile_wgs + p.few_wgs > 0x7FFFFFFFl / (64 * kWaves) || q.max_len > (long)p.max_parts * p.per_split * kPage || p.call_parts < 1 ||
-        (long)p.call_parts * p.per_split * kPage < q.max_len || (long)q.B * a.Hkv > 0x7FFFFFFFl / 4096 ||
+        (long)p.tile_wgs + p.few_wgs > 0xFFFFFFFFl / (64 * kWaves) || q.max_len > (long)p.max_parts * p.per_split * kPage || p.call_parts < 1 ||
+        (long)p.call_parts * p.per_split * kPage < q.max_len || (long)q.B * a.Hkv > kPagedMaxPairs ||
         (long)p.max_parts * p.per_split > 0x7FFFFFFFl / kPage || !a.part ||
         ((long)q.max_q * group > kPagedFewRows && p.tile_wgs < std::max<long>(most_tiles(a.H, a.Hkv, q.rows, q.B) * a.Hkv, kPagedTileParts)))
         return hipErrorInvalidValue;

@@ -44,13 +44,14 @@ def test_destroying_nothing():
 @pytest.mark.parametrize("field,value,code", [
     ("n_heads", 0, -1), ("n_kv_heads", 0, -1), ("n_kv_heads", 3, -1), ("n_kv_heads", 16, -1), ("head_dim", 96, -5), ("dtype", 2, -1),
     ("n_pages", 0, -1), ("max_rows", 0, -1), ("max_batch", 0, -1), ("max_ctx", 0, -1), ("max_ctx", (1 << 24) + 1, -5),
-    ("max_batch", 4097, -5), ("max_rows", (1 << 20) + 1, -5), ("n_heads", 2048, -5)])
+    ("max_batch", 4097, -5), ("max_rows", (1 << 20) + 1, -5), ("n_heads", 2048, -5), ("wide", (1024, 1024, 1024), -5)])
 def test_configs_that_are_refused(field, value, code):
+    kw = dict(zip(("n_heads", "n_kv_heads", "max_batch"), value)) if field == "wide" else {field: value}
     with pytest.raises(B.SdsatError) as e:
-        B.sdsat_paged_query_sizes(config(**{field: value}))
+        B.sdsat_paged_query_sizes(config(**kw))
     assert e.value.code == code
     out = ctypes.c_void_p()
-    assert B.lib().sdsat_paged_init(ctypes.byref(config(**{field: value})), 256, 1 << 40, None, ctypes.byref(out)) == code
+    assert B.lib().sdsat_paged_init(ctypes.byref(config(**kw)), 256, 1 << 40, None, ctypes.byref(out)) == code
     assert out.value is None
 
 
