@@ -214,7 +214,7 @@ struct PagedAppendArgs {
 hipError_t launch_paged_append(int dtype, int x_dtype, int head_dim, const PagedAppendArgs& a, hipStream_t s);
 
 // Attention.  Rows of the H / Hkv query heads that share a key head are packed, row i * group + head.  Sequences of up to
-// kPagedFewRows packed rows are cut into parts of per_split pages, counted from slot 0, longer ones into tiles of
+// kPagedFewRows packed rows are cut into parts of 2^part_shift pages, counted from slot 0, longer ones into tiles of
 // kPagedTileRows packed rows, and each tile's pages into parts where there are few tiles.
 constexpr int kPagedFewRows = 64, kPagedTileRows = 128;
 constexpr int kPagedMaxPairs = 1 << 19;  // sequences and key heads of a call (a launch's 2^32 threads)
@@ -222,8 +222,9 @@ constexpr int kPagedMaxParts = 64;       // parts of a short chunk, at most
 constexpr int kPagedMaxTileParts = 16;   // parts of a tile, at most
 constexpr int kPagedTileParts = 512;    // of all tiles and key heads, at most, where tiles have several
 struct PagedPlan {
-    int per_split, max_parts;            // of the handle
+    int part_shift, max_parts;           // of the handle
     int tile_wgs, few_wgs, call_parts;   // of a call: workgroups; parts of a short chunk, at most
+    int few_once;                        // ... whether every piece of the short chunks has a workgroup
 };
 struct PagedAttnArgs {
     PagedSeqs seq;
@@ -233,11 +234,11 @@ struct PagedAttnArgs {
     void* out; long ldo; int out_f32;
     int H, Hkv, window;      // window 0: none
     float scale;             // times log2 e
-    int per_split, max_parts, tile_wgs, few_wgs;
+    int part_shift, max_parts, tile_wgs, few_wgs, few_once;
     float* part;             // short chunks' parts [B][Hkv][max_parts][kPagedFewRows][Dh + 4], then the tiles'
     size_t tile_part;        // where those begin
 };
-// per_split and max_parts: of the configuration alone, so that a row's sums do not follow what else is in its call
+// part_shift and max_parts: of the configuration alone, so that a row's sums do not follow what else is in its call
 PagedPlan plan_paged(int Hkv, int max_batch, int max_ctx);
 // ... and a call's part of the plan
 void plan_paged_call(PagedPlan& p, int H, int Hkv, int B, int rows, int max_q, int max_len);

@@ -223,7 +223,7 @@ int sdsat_paged_attention(sdsat_paged* p, const sdsat_paged_batch* batch, const 
     a.kp = d_k; a.vp = d_v; a.q = d_q; a.ldq = ld_q; a.mask = d_mask; a.out = d_out; a.ldo = ld_out;
     a.out_f32 = out_dtype == SDSAT_DTYPE_FP32;
     a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.window = window; a.scale = in2;
-    a.per_split = plan.per_split; a.max_parts = plan.max_parts; a.tile_wgs = plan.tile_wgs; a.few_wgs = plan.few_wgs;
+    a.part_shift = plan.part_shift; a.max_parts = plan.max_parts; a.tile_wgs = plan.tile_wgs; a.few_wgs = plan.few_wgs; a.few_once = plan.few_once;
     a.part = p->part; a.tile_part = p->tile_part;
     return launched(p, launch_paged_attention(c.dtype, c.head_dim, plan, a, p->stream), "paged attention");
 }

@@ -19,7 +19,7 @@
 //  * short chunks, up to kPagedFewRows packed rows: 32 rows and a part of the sequence's pages, which the waves take in
 //    turn; a wave's page goes into its own piece of LDS, K's half while the page before is weighed with V, V's half while
 //    the next scores are formed; no barriers.  The waves' results are joined by log-sum-exp in wave order.
-// A chunk's part is per_split pages from a slot that is a multiple of them, the same for the handle's every call: a row's
+// A chunk's part is 2^part_shift pages from a slot that is a multiple of them, the same for the handle's every call: a row's
 // result does not depend on what else is in its call, nor on the chunk's other rows while there are at most kPagedFewRows
 // packed ones.  Results of parts go to scratch; a second launch joins them (in the workgroup that comes last it took longer:
 // 11 rows of 8 sequences over 3000 slots 47 us, 39 so).
@@ -385,18 +385,25 @@ __device__ __forceinline__ void put4(__amdgpu_buffer_rsrc_t r, uint32_t off, f32
 }
 
 // packed rows row0 .. row0 + rows - 1 of a chunk and key head
-struct Rows { int b, h, row0, rows, group; PagedSeq seq; };
+struct Rows {
+    int b, h, row0, rows, group;
+    PagedSeq seq;
+    uint32_t inv;   // of short chunks: ceil(2^16 / group); 0: divide
+    // the chunk's row of packed row p (p + 1 <= kPagedFewRows where inv is given: then p * inv < 2^16 (p / group + 1))
+    __device__ __forceinline__ int row(int p) const { return inv ? (int)(((uint32_t)p * inv) >> 16) : p / group; }
+};
 
 template <typename T, int DH>
-__device__ __forceinline__ const T* q_row(const PagedAttnArgs& a, const Rows& r, int i) {
-    const int p = r.row0 + min(i, r.rows - 1);
-    return reinterpret_cast<const T*>(a.q) + (size_t)(r.seq.start + p / r.group) * a.ldq + (size_t)(r.h * r.group + p % r.group) * DH;
+__device__ __forceinline__ const T* q_row(const PagedAttnArgs& a, const Rows& r, int n) {
+    const int p = r.row0 + min(n, r.rows - 1);
+    const int i = r.row(p);
+    return reinterpret_cast<const T*>(a.q) + (size_t)(r.seq.start + i) * a.ldq + (size_t)(r.h * r.group + p - i * r.group) * DH;
 }
 
 template <typename T, int DH>
-__device__ __forceinline__ void store_row(const PagedAttnArgs& a, const Rows& r, int i, int d, f32x4_t v) {
-    const int p = r.row0 + i;
-    const size_t off = (size_t)(r.seq.start + p / r.group) * a.ldo + (size_t)(r.h * r.group + p % r.group) * DH + d;
+__device__ __forceinline__ void store_row(const PagedAttnArgs& a, const Rows& r, int n, int d, f32x4_t v) {
+    const int p = r.row0 + n, i = r.row(p);
+    const size_t off = (size_t)(r.seq.start + i) * a.ldo + (size_t)(r.h * r.group + p - i * r.group) * DH + d;
     if (sizeof(T) == 4 || a.out_f32) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + off) = v;
     else *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + off) = uint2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
 }
@@ -405,8 +412,8 @@ template <typename T, int DH>
 __device__ __forceinline__ Sight sight_of(const PagedAttnArgs& a, const Rows& r, int w0, int lane) {
     Sight s;
     const int end = r.rows - 1;   // rows past it, and those of a wave that has none, look like the last
-    const int i = (r.row0 + min(w0 + (lane & 31), end)) / r.group;
-    const int i0 = (r.row0 + min(w0, end)) / r.group, i1 = (r.row0 + min(w0 + 31, end)) / r.group;
+    const int i = r.row(r.row0 + min(w0 + (lane & 31), end));
+    const int i0 = r.row(r.row0 + min(w0, end)), i1 = r.row(r.row0 + min(w0 + 31, end));
     s.tree = a.mask != nullptr;
     s.len = r.seq.len;
     s.first = a.window && !s.tree ? max(0, r.seq.len + i - a.window + 1) : 0;
@@ -466,12 +473,23 @@ __device__ __forceinline__ int count_pieces(const PagedSeqs& s, int lane, F piec
     return __builtin_amdgcn_readfirstlane(all);
 }
 
-// Pages lo .. hi - 1 that packed rows row0 .. see between them.
-__device__ __forceinline__ void page_range(const PagedAttnArgs& a, const Rows& r, int& lo, int& hi) {
-    const int i0 = r.row0 / r.group, i1 = (r.row0 + r.rows - 1) / r.group;
+// Pages lo .. hi - 1 that the chunk's rows i0 .. i1 see between them.
+__device__ __forceinline__ void page_range(const PagedAttnArgs& a, const PagedSeq& q, int i0, int i1, int& lo, int& hi) {
     const bool tree = a.mask != nullptr;
-    lo = a.window && !tree ? max(0, r.seq.len + i0 - a.window + 1) / kPage : 0;
-    hi = (r.seq.len + (tree ? r.seq.n - 1 : i1)) / kPage + 1;
+    lo = a.window && !tree ? max(0, q.len + i0 - a.window + 1) / kPage : 0;
+    hi = (q.len + (tree ? q.n - 1 : i1)) / kPage + 1;
+}
+__device__ __forceinline__ void page_range(const PagedAttnArgs& a, const Rows& r, int& lo, int& hi) {
+    page_range(a, r.seq, r.row(r.row0), r.row(r.row0 + r.rows - 1), lo, hi);
+}
+// A short chunk: its pages, its first part and their number.
+struct FewParts { int lo, hi, first, parts; };
+__device__ __forceinline__ FewParts few_parts(const PagedAttnArgs& a, const PagedSeq& q) {
+    FewParts f;
+    page_range(a, q, 0, q.n - 1, f.lo, f.hi);
+    f.first = f.lo >> a.part_shift;
+    f.parts = ((f.hi - 1) >> a.part_shift) - f.first + 1;
+    return f;
 }
 
 // ------------------------------------------------------------------ short chunks
@@ -490,8 +508,8 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
     RowWave<T, DH, 1> w;
     w.clear();
     const Sight see = sight_of<T, DH>(a, r, 0, lane);
-    const int begin = sp * a.per_split;
-    const int from = max(lo, begin), to = min(hi, begin + a.per_split);
+    const int begin = sp << a.part_shift;
+    const int from = max(lo, begin), to = min(hi, begin + (1 << a.part_shift));
     const int first = begin + (from - begin + 3 - wave) / kWaves * kWaves + wave;   // this wave's first page
     const int cnt = first < to ? (to - first + kWaves - 1) / kWaves : 0;
     unsigned char* s_k = smem + wave * P::BLK;
@@ -592,28 +610,22 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
 template <typename T, int DH>
 __device__ __forceinline__ void few_work(const PagedAttnArgs& a, int wg, int wgs, unsigned char* smem, int wave, int lane) {
     const int group = a.H / a.Hkv;
-    auto whole = [&](const PagedSeq& q) { return Rows{0, 0, 0, q.n * group, group, q}; };
     auto pieces = [&](const PagedSeq& q) {
-        if (q.n == 0 || q.n * (long)group > kPagedFewRows) return 0;
-        int lo, hi;
-        page_range(a, whole(q), lo, hi);
-        return ((hi - 1) / a.per_split - lo / a.per_split + 1) * ((q.n * group + 31) / 32) * a.Hkv;
+        return q.n == 0 || q.n * (long)group > kPagedFewRows ? 0 : few_parts(a, q).parts * ((q.n * group + 31) / 32) * a.Hkv;
     };
     for (int want = wg;; want += wgs) {
         const Found f = find_piece(a.seq, want, lane, pieces);
         if (!f.ok) return;
-        Rows r = whole(f.seq);
-        int lo, hi;
-        page_range(a, r, lo, hi);
-        const int sp0 = lo / a.per_split, parts = (hi - 1) / a.per_split - sp0 + 1, tiles = (r.rows + 31) / 32;
-        r.b = f.b;
-        r.h = f.k % a.Hkv;
-        r.row0 = f.k / a.Hkv % tiles * 32;
-        r.rows = min(32, r.rows - r.row0);
-        few_rows<T, DH>(a, r, lo, hi, sp0 + f.k / a.Hkv / tiles, sp0, parts, smem, wave, lane);
+        const FewParts fp = few_parts(a, f.seq);
+        const int two = f.seq.n * group > 32, k = f.k / a.Hkv;   // 32 rows or twice
+        Rows r{f.b, f.k - k * a.Hkv, (k & two) * 32, 0, group, f.seq, (65535u + group) / group};
+        r.rows = min(32, f.seq.n * group - r.row0);
+        few_rows<T, DH>(a, r, fp.lo, fp.hi, fp.first + (k >> two), fp.first, fp.parts, smem, wave, lane);
+        if (a.few_once) return;
         __syncthreads();   // smem is free
     }
 }
+static_assert(kPagedFewRows == 64, "a short chunk is 32 rows or twice");
 
 // ------------------------------------------------------------------ tiles
 // Where rows 32 sub .. of a tile's part go.
@@ -637,7 +649,7 @@ __device__ __forceinline__ TileWork tile_work(const PagedAttnArgs& a, int want, 
     const int h = f.k % a.Hkv, nth = f.k / a.Hkv / each;
     t.sp = f.k / a.Hkv % each;
     t.slot = (want - f.k) / each + nth * a.Hkv + h;
-    t.r = Rows{f.b, h, (tiles_of(f.seq) - 1 - nth) * kPagedTileRows, 0, group, f.seq};   // the longest first
+    t.r = Rows{f.b, h, (tiles_of(f.seq) - 1 - nth) * kPagedTileRows, 0, group, f.seq, 0};   // the longest first
     t.r.rows = min(kPagedTileRows, f.seq.n * group - t.r.row0);
     page_range(a, t.r, t.lo, t.hi);
     const int per = max((t.hi - t.lo + t.splits - 1) / t.splits, 4);
@@ -807,17 +819,12 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a, int fe
     if (x < few) {
         const int slice = x % slices;
         x /= slices;
-        Rows r{0, 0, x % subs * 32, 0, group, {}};
+        const int sub = x % subs;
         x /= subs;
-        r.h = x % a.Hkv;
-        r.b = x / a.Hkv;
-        r.seq = load_seq(a.seq, r.b);
-        const int rows = r.seq.n * group;
-        if (rows <= r.row0 || rows > kPagedFewRows) return;
-        int lo, hi;
-        page_range(a, Rows{r.b, 0, 0, rows, group, r.seq}, lo, hi);
-        const int parts = (hi - 1) / a.per_split - lo / a.per_split + 1;
-        if (parts < 2) return;
+        const int b = x / a.Hkv;
+        Rows r{b, x - b * a.Hkv, sub * 32, 0, group, load_seq(a.seq, b), (65535u + group) / group};
+        const int rows = r.seq.n * group, parts = r.seq.n ? few_parts(a, r.seq).parts : 0;
+        if (rows <= r.row0 || rows > kPagedFewRows || parts < 2) return;
         r.rows = min(32, rows - r.row0);
         join_parts<T, DH>(a, r, reinterpret_cast<const f32x4_t*>(few_part<DH>(a, r, 0)), kPagedFewRows / 32 * kPartFloats<DH> / 4, parts,
                           slice, slices, s_w);
@@ -859,9 +866,11 @@ PagedPlan plan_paged(int Hkv, int max_batch, int max_ctx) {
     // token over 1500 slots of 8 key heads 15.1, 14.1, 15.1; 6 tokens of 4 sequences over 3000 37, 26, 20; 64 tokens over 500
     // slots 39, 39, 26; 11 rows of 4 sequences over 1500 slots of 32 heads 33, 31, 28.  512 to 4096 parts, 64 tokens over 4000
     // slots: 167, 167, 173, 181.
-    long per = std::max<long>(16, std::min<long>((cap * pairs + 1023) / 1024, 64));
-    per = std::max(per, (cap + kPagedMaxParts - 1) / kPagedMaxParts);
-    p.per_split = (int)per;
+    // (A power of two, as the kernels shift, near the number, and enough of them for a full cache in kPagedMaxParts.)
+    const long want = std::min<long>((cap * pairs + 1023) / 1024, 64), least = (cap + kPagedMaxParts - 1) / kPagedMaxParts;
+    p.part_shift = 4;
+    while ((2l << p.part_shift) * 3 <= want * 4 || (1l << p.part_shift) < least) ++p.part_shift;
+    const long per = 1l << p.part_shift;
     p.max_parts = (int)((cap + per - 1) / per);
     return p;
 }
@@ -875,9 +884,11 @@ void plan_paged_call(PagedPlan& p, int H, int Hkv, int B, int rows, int max_q, i
     if ((long)max_q * group > kPagedFewRows)
         p.tile_wgs = (int)std::min<long>(std::max<long>(most_tiles(H, Hkv, rows, B) * Hkv, kPagedTileParts), 0x7FFFFFFF);
     const int tiles = (int)std::min<long>(((long)max_q * group + 31) / 32, kPagedFewRows / 32);
-    const long parts = ((long)max_len + kPage * p.per_split - 1) / (kPage * p.per_split);
+    const long parts = ((long)max_len + ((long)kPage << p.part_shift) - 1) / ((long)kPage << p.part_shift);
     p.call_parts = (int)parts;
-    p.few_wgs = (int)std::max<long>(1, std::min<long>(parts * B * tiles * Hkv, 2048));
+    const long pieces = parts * B * tiles * Hkv;
+    p.few_wgs = (int)std::max<long>(1, std::min<long>(pieces, 2048));
+    p.few_once = pieces <= p.few_wgs;
 }
 
 size_t paged_part_floats(const PagedPlan& p, int H, int Hkv, int head_dim, int max_batch, int max_rows, size_t* tile_part) {
@@ -905,12 +916,12 @@ hipError_t launch_paged_attention(int dtype, int head_dim, const PagedPlan& p, c
     const int group = a.Hkv > 0 ? a.H / a.Hkv : 0;
     if (group < 1 || a.H % a.Hkv || q.B < 1 || q.rows < 0 || q.pages_ld < 1 || q.n_pages < 1 || q.max_q < 0 || q.max_len < 0 ||
         q.max_len > (long)q.pages_ld * kPage || !q.start || !q.len || !q.pages || !q.err || !a.kp || !a.vp || !a.q || !a.out ||
-        (a.mask && (q.max_q > 64 || a.window)) || a.window < 0 || !(a.scale > 0.f) || a.ldq % 8 || a.ldo % 4 || p.per_split < 1 ||
-        a.per_split != p.per_split || a.tile_wgs != p.tile_wgs || a.few_wgs != p.few_wgs || a.max_parts != p.max_parts ||
+        (a.mask && (q.max_q > 64 || a.window)) || a.window < 0 || !(a.scale > 0.f) || a.ldq % 8 || a.ldo % 4 || p.part_shift < 0 || p.part_shift > 20 ||
+        a.part_shift != p.part_shift || a.few_once != p.few_once || a.tile_wgs != p.tile_wgs || a.few_wgs != p.few_wgs || a.max_parts != p.max_parts ||
         p.few_wgs < 1 || p.max_parts > kPagedMaxParts ||
-        (long)p.tile_wgs + p.few_wgs > 0xFFFFFFFFl / (64 * kWaves) || q.max_len > (long)p.max_parts * p.per_split * kPage || p.call_parts < 1 ||
-        (long)p.call_parts * p.per_split * kPage < q.max_len || (long)q.B * a.Hkv > kPagedMaxPairs ||
-        (long)p.max_parts * p.per_split > 0x7FFFFFFFl / kPage || !a.part ||
+        (long)p.tile_wgs + p.few_wgs > 0xFFFFFFFFl / (64 * kWaves) || q.max_len > ((long)p.max_parts * kPage << p.part_shift) || p.call_parts < 1 ||
+        ((long)p.call_parts * kPage << p.part_shift) < q.max_len || (long)q.B * a.Hkv > kPagedMaxPairs ||
+        ((long)p.max_parts << p.part_shift) > 0x7FFFFFFFl / kPage || !a.part ||
         ((long)q.max_q * group > kPagedFewRows && p.tile_wgs < std::max<long>(most_tiles(a.H, a.Hkv, q.rows, q.B) * a.Hkv, kPagedTileParts)))
         return hipErrorInvalidValue;
     if (dtype == 1) {

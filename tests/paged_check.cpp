@@ -26,8 +26,8 @@ int main() {
     for (const Cfg& c : cfgs) {
         const PagedPlan p = plan_paged(c.Hkv, c.B, c.ctx);
         const int group = c.H / c.Hkv;
-        CHECK(p.per_split >= 4 && p.max_parts >= 1 && p.max_parts <= kPagedMaxParts && (long)p.max_parts * p.per_split * kPage >= c.ctx,
-              "parts: %d of %d pages for %d slots", p.max_parts, p.per_split, c.ctx);
+        CHECK(p.part_shift >= 4 && p.max_parts >= 1 && p.max_parts <= kPagedMaxParts && ((long)p.max_parts * kPage << p.part_shift) >= c.ctx,
+              "parts: %d of 2^%d pages for %d slots", p.max_parts, p.part_shift, c.ctx);
         size_t tile_at = 0;
         const size_t have = paged_part_floats(p, c.H, c.Hkv, c.Dh, c.B, c.rows, &tile_at);
         for (int B = 1; B <= c.B; B += 1 + B / 3)
@@ -35,8 +35,8 @@ int main() {
                 for (long rows = max_q; rows <= c.rows; rows += 1 + rows) {
                     PagedPlan q = p;
                     plan_paged_call(q, c.H, c.Hkv, B, (int)rows, (int)max_q, c.ctx);
-                    CHECK(q.per_split == p.per_split && q.max_parts == p.max_parts, "a call moves the handle's parts");
-                    CHECK(q.few_wgs >= 1 && (long)q.call_parts * q.per_split * kPage >= c.ctx && q.call_parts <= q.max_parts,
+                    CHECK(q.part_shift == p.part_shift && q.max_parts == p.max_parts, "a call moves the handle's parts");
+                    CHECK(q.few_wgs >= 1 && ((long)q.call_parts * kPage << q.part_shift) >= c.ctx && q.call_parts <= q.max_parts,
                           "short chunks: %d workgroups, %d parts", q.few_wgs, q.call_parts);
                     // tiles: every sequence may end in one that is not full
                     const bool tiles = max_q * group > kPagedFewRows;
@@ -85,7 +85,8 @@ int main() {
     at.out = mem;
     at.part = reinterpret_cast<float*>(mem);
     at.ldq = at.ldo = 128; at.H = 2; at.Hkv = 1; at.scale = 1.f;
-    at.per_split = plan.per_split; at.max_parts = plan.max_parts; at.tile_wgs = plan.tile_wgs; at.few_wgs = plan.few_wgs;
+    at.part_shift = plan.part_shift; at.max_parts = plan.max_parts; at.tile_wgs = plan.tile_wgs; at.few_wgs = plan.few_wgs;
+    at.few_once = plan.few_once;
     auto attend = [&](const char* what, auto change) {
         PagedAttnArgs a = at;
         PagedPlan p = plan;
@@ -104,8 +105,8 @@ int main() {
     attend("attention: mask with a window", [](A a, P, int&) { static uint64_t m; a.mask = &m; a.window = 3; });
     attend("attention: mask of long chunks", [](A a, P, int&) { static uint64_t m; a.mask = &m; a.seq.max_q = 65; });
     attend("attention: H % Hkv", [](A a, P, int&) { a.H = 3; a.Hkv = 2; });
-    attend("attention: another plan's parts", [](A a, P, int&) { a.per_split += 1; });
-    attend("attention: parts too short", [](A a, P p, int&) { a.per_split = p.per_split = 1; a.max_parts = p.max_parts = 1; });
+    attend("attention: another plan's parts", [](A a, P, int&) { a.part_shift += 1; });
+    attend("attention: parts too short", [](A a, P p, int&) { a.part_shift = p.part_shift = 0; a.max_parts = p.max_parts = 1; });
     attend("attention: tiles that the plan lacks", [](A a, P, int&) { a.seq.max_q = a.seq.rows = 33; });
     attend("attention: ldq % 8", [](A a, P, int&) { a.ldq = 132; });
 
