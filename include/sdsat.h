@@ -390,10 +390,11 @@ int sdsat_paged_append(sdsat_paged* paged, const sdsat_paged_batch* batch, void*
  * them (s among them).  With d_mask ([rows] uint64, max_q <= 64, no window) it sees the slots below
  * d_len and of its chunk's rows j those with bit j set.  A row that sees nothing gives zeros.
  * scale 0: 1 / sqrt(head_dim).  d_out: [rows, ld_out], the pool's type or fp32.  Scores, sums and
- * outputs are accumulated in float; the weights are rounded to the pool's type.  A row's result
- * depends on its sequence alone, not on the rest of the call; while a chunk has at most 64 query heads
- * per key head and token (rows * n_heads / n_kv_heads <= 64) nor on the chunk's length: a token decoded
- * alone and the same token in a draft block give the same bits.  Stream-ordered. */
+ * outputs are accumulated in float; the weights are rounded to the pool's type.  While a chunk has
+ * rows * n_heads / n_kv_heads <= 64, its rows' results depend, for one handle configuration, neither on
+ * the rest of the call nor on the chunk's length: a token decoded alone and the same token in a draft
+ * block give the same bits.  Longer chunks are summed in an order that the call's number of rows
+ * decides; the same call gives the same bits.  Stream-ordered. */
 int sdsat_paged_attention(sdsat_paged* paged, const sdsat_paged_batch* batch, const void* d_k,
                           const void* d_v, const void* d_q, int64_t ld_q, const uint64_t* d_mask,
                           int32_t window, float scale, void* d_out, int32_t out_dtype, int64_t ld_out);

@@ -13,9 +13,9 @@
 // heads forms its 4 sines once; U heads' columns are on their way at once.  K's rows are written whole.  V's lie transposed
 // in a page (32 slots beside each other for one column): pages of more than kScatterTokens new tokens are turned in LDS and
 // written 16 bytes at a time where all of a chunk's slots are new; fewer tokens are written element by element.
-// Bound by memory, and by latency for single tokens: 4 prompts of 2047 tokens, 48 heads of 128 in bf16 (201 MB) 55 us,
-// 3.6 TB/s (a large copy 4.9; without the norms 51, one head at a time 73); one token of 64 sequences 8.1 us, a block of 6
-// tokens of the tiny decoder 6.5 (a launch that does nothing about 4).
+// Bound by memory, and by latency for single tokens: 4 prompts of 2047 tokens, 48 heads of 128 in bf16 (201 MB) 54 us,
+// 3.7 TB/s (a large copy 4.9; without the norms 51, one head at a time 73); one token of 64 sequences 8.4 us, a block of 6
+// tokens of the tiny decoder 6.7 (a call cannot take less than the host's launch, 4.4).
 #include <algorithm>
 
 #include "paged_device.h"

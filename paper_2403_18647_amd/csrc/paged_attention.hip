@@ -19,10 +19,18 @@
 //  * short chunks, up to kPagedFewRows packed rows: 32 rows and a part of the sequence's pages, which the waves take in
 //    turn; a wave's page goes into its own piece of LDS, K's half while the page before is weighed with V, V's half while
 //    the next scores are formed; no barriers.  The waves' results are joined by log-sum-exp in wave order.
-// A chunk's part is 2^part_shift pages from a slot that is a multiple of them, the same for the handle's every call: a row's
-// result does not depend on what else is in its call, nor on the chunk's other rows while there are at most kPagedFewRows
-// packed ones.  Results of parts go to scratch; a second launch joins them (in the workgroup that comes last it took longer:
+// A short chunk's part is 2^part_shift pages from a slot that is a multiple of them, the same for the handle's every call:
+// a row's result depends neither on what else is in its call nor on the chunk's other rows.  Tiles are in as many parts as
+// the call's number of them leaves room for, so that their results depend on it in the order of summation.  Results of parts go to scratch; a second launch joins them (in the workgroup that comes last it took longer:
 // 11 rows of 8 sequences over 3000 slots 47 us, 39 so).
+//
+// Bound by memory where rows are few: a token each of 64 sequences of up to 4000 slots, 8 key heads of 128 in bf16 (893 MB),
+// 143 us, 6.2 TB/s; of one of 130000 (533 MB) 87, 6.1; and by the way to the first page and the second launch where slots
+// are few too (11 rows each of 4 sequences of 1500, 98 MB: 26 us, 14 at the rate of a read stream).  Long chunks are bound
+// by the matrix cores at the clock that the card holds under them: 4096 rows behind 4096 slots, 32 heads, 412 GFLOP, 423 us,
+// 975 TFLOP/s (a large product 1180 to 1230); the matrix pipes are busy 49% of the cycles, and without the softmax, or
+// without loads and barriers, it took about a tenth less.  A chunk of 1001 rows beside 31 single tokens: 166 us, 74 at
+// both rates.
 #include <algorithm>
 #include <type_traits>
 
@@ -37,7 +45,6 @@ __device__ __forceinline__ int tile_splits(int tiles, int Hkv) {
     return max(1, min(kPagedMaxTileParts, kPagedTileParts / max(1, tiles * Hkv)));
 }
 static constexpr int kWaves = 4;
-static constexpr int kTileSlices = 1;   // workgroups that join 32 rows of a tile, each some of the columns
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
@@ -831,14 +838,14 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a, int fe
         return;
     }
     x -= few;
-    const int slice = x % kTileSlices, sub = x / kTileSlices % (kPagedTileRows / 32);
-    const TileWork t = tile_work(a, x / kTileSlices / (kPagedTileRows / 32), true, lane);
+    const int sub = x % (kPagedTileRows / 32);
+    const TileWork t = tile_work(a, x / (kPagedTileRows / 32), true, lane);
     if (!t.ok || t.parts < 2 || 32 * sub >= t.r.rows) return;
     Rows r = t.r;
     r.row0 += 32 * sub;
     r.rows = min(32, r.rows - 32 * sub);
     join_parts<T, DH>(a, r, reinterpret_cast<const f32x4_t*>(tile_part<DH>(a, t.slot * t.splits, sub)),
-                      kPagedTileRows / 32 * kPartFloats<DH> / 4, t.parts, slice, kTileSlices, s_w);
+                      kPagedTileRows / 32 * kPartFloats<DH> / 4, t.parts, 0, 1, s_w);
 }
 
 // ------------------------------------------------------------------ the launch
@@ -906,7 +913,7 @@ static hipError_t launch_dh(const PagedPlan& p, const PagedAttnArgs& a, hipStrea
     // tiles in several parts are kPagedTileParts / 2 at the most, with key heads
     const int subs = (long)a.seq.max_q * (a.H / a.Hkv) > 32 ? kPagedFewRows / 32 : 1, slices = p.call_parts > 8 ? 4 : 1;
     const int few = p.call_parts > 1 ? a.seq.B * a.Hkv * subs * slices : 0;
-    const int join = few + (p.tile_wgs ? kPagedTileParts / 2 * (kPagedTileRows / 32) * kTileSlices : 0);
+    const int join = few + (p.tile_wgs ? kPagedTileParts / 2 * (kPagedTileRows / 32) : 0);
     if (join) hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3((unsigned)join), dim3(256), 0, s, a, few, subs, slices);
     return hipGetLastError();
 }
