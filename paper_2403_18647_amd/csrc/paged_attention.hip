@@ -318,9 +318,11 @@ struct RowWave {
             const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
             top = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * scale;   // scale > 0
         }
-        if (__any((top > base + kRaise) | ((base == -INFINITY) & (top > base)))) {
-            const float to = fmaxf(base, top);
-            const float alpha = base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - to);
+        // each row for itself: what the wave's other rows do must not move its base, which its weights are rounded to
+        const bool raise = (top > base + kRaise) | ((base == -INFINITY) & (top > base));
+        if (__any(raise)) {
+            const float to = raise ? top : base;   // top > base
+            const float alpha = !raise ? 1.f : base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - to);
             sum *= alpha;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
