@@ -760,20 +760,24 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
 
 // ------------------------------------------------------------------ joining parts
 // Parts 0 .. n - 1 of rows (at most 32) joined by log-sum-exp, part p's at part + p * stride quads; columns
-// of slice `slice` of `slices`.  Even parts in order, odd ones in order, then both: half a wave each.
+// of slice `slice` of `slices`.  Even parts in order, odd ones in order, then both: half a wave each.  Parts that a row sees
+// nothing of add zeros, and the sums are taken over lanes that stand for the sequence's parts from its beginning (the first
+// here is its part `first`): a row's bits do not depend on which parts the chunk's other rows see.
 template <typename T, int DH>
-__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Rows& r, const f32x4_t* part, int stride, int n, int slice,
-                                           int slices, float (*s_w)[32]) {
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Rows& r, const f32x4_t* part, int stride, int first, int n,
+                                           int slice, int slices, float (*s_w)[32]) {
     constexpr int D4 = DH / 4;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     static_assert(kPagedMaxParts <= 64, "a lane for each part");
     // a row's bases and sums in the lanes of a wave; the waves take the rows in turn
+    const int p = lane - first;
+    const bool mine = p >= 0 && p < n;
     for (int i = tid / 64; i < r.rows; i += 4) {
-        const f32x4_t v = part[(size_t)min(lane, n - 1) * stride + D4 * r.rows + i];
-        const float m = lane < n ? v[0] : -INFINITY, top = across_wave(m, OpMax());
+        const f32x4_t v = part[(size_t)min(max(p, 0), n - 1) * stride + D4 * r.rows + i];
+        const float m = mine ? v[0] : -INFINITY, top = across_wave(m, OpMax());
         const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-        const float den = across_wave(lane < n ? w * v[1] : 0.f, OpSum());
-        if (lane < n) s_w[lane][i] = w * (den == 0.f ? 0.f : 1.0f / den);
+        const float den = across_wave(mine ? w * v[1] : 0.f, OpSum());
+        if (mine) s_w[p][i] = w * (den == 0.f ? 0.f : 1.0f / den);
     }
     __syncthreads();
     const int quads = r.rows * (D4 / slices);
@@ -832,11 +836,13 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a, int fe
         x /= subs;
         const int b = x / a.Hkv;
         Rows r{b, x - b * a.Hkv, sub * 32, 0, group, load_seq(a.seq, b), (65535u + group) / group};
-        const int rows = r.seq.n * group, parts = r.seq.n ? few_parts(a, r.seq).parts : 0;
-        if (rows <= r.row0 || rows > kPagedFewRows || parts < 2) return;
+        const int rows = r.seq.n * group;
+        if (rows <= r.row0 || rows > kPagedFewRows) return;
+        const FewParts fp = few_parts(a, r.seq);
+        if (fp.parts < 2) return;
         r.rows = min(32, rows - r.row0);
-        join_parts<T, DH>(a, r, reinterpret_cast<const f32x4_t*>(few_part<DH>(a, r, 0)), kPagedFewRows / 32 * kPartFloats<DH> / 4, parts,
-                          slice, slices, s_w);
+        join_parts<T, DH>(a, r, reinterpret_cast<const f32x4_t*>(few_part<DH>(a, r, 0)), kPagedFewRows / 32 * kPartFloats<DH> / 4,
+                          fp.first, fp.parts, slice, slices, s_w);
         return;
     }
     x -= few;
@@ -847,7 +853,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a, int fe
     r.row0 += 32 * sub;
     r.rows = min(32, r.rows - 32 * sub);
     join_parts<T, DH>(a, r, reinterpret_cast<const f32x4_t*>(tile_part<DH>(a, t.slot * t.splits, sub)),
-                      kPagedTileRows / 32 * kPartFloats<DH> / 4, t.parts, 0, 1, s_w);
+                      kPagedTileRows / 32 * kPartFloats<DH> / 4, 0, t.parts, 0, 1, s_w);
 }
 
 // ------------------------------------------------------------------ the launch

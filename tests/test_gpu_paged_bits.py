@@ -19,23 +19,23 @@ def _gpu():
 HEADS = [("bf16", 4, 4, 128), ("bf16", 8, 2, 64), ("bf16", 7, 1, 128), ("fp32", 2, 2, 64), ("fp32", 6, 2, 128)]
 
 
-def alone(c, b, i, q, window=0, mask=None):
+def alone(c, b, i, q, window=0, out_type=None):
     """Row i of sequence b of a call as a call of its own, on the same handle and pages."""
     row, slot = c.start[b] + i, c.seqs[b][1] + i
     t = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
-    out = torch.zeros_like(q[:1])
+    out = torch.zeros_like(q[:1], dtype=out_type or q.dtype)
     B.sdsat_paged_attention(c.handle, B.paged_batch(t([0, 1]), t([slot]), c.pages[b:b + 1], 1, 1, slot + 1), c.k, c.v,
-                            q[row:row + 1].contiguous(), mask, window, 0.0, out)
+                            q[row:row + 1].contiguous(), None, window, 0.0, out)
     return out[0]
 
 
-def assert_rows_alone(c, q, window=0, mask=None):
-    got = c.attend(q, mask=mask, window=window)
+def assert_rows_alone(c, q, window=0, out_type=None):
+    got = c.attend(q, window=window, out=torch.zeros_like(q, dtype=out_type or q.dtype))
     B.sdsat_paged_status(c.handle)
     for b, (n, _) in enumerate(c.seqs):
         assert n * (c.heads // c.kv) <= 64
         for i in range(n):
-            same = torch.equal(got[c.start[b] + i], alone(c, b, i, q, window))
+            same = torch.equal(got[c.start[b] + i], alone(c, b, i, q, window, out_type))
             assert same, f"row {i} of sequence {b}"
     return got
 
@@ -70,3 +70,35 @@ def test_windows_that_begin_on_both_sides_of_a_page(dtype, heads, kv, dh, window
     q = c.randn((c.rows, heads * dh), scale=2.0)
     got = assert_rows_alone(c, q, window)
     assert_within(got, *c.expected(q, window=window))
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dh", HEADS)
+@pytest.mark.parametrize("window", [1400, 2900])
+def test_windows_that_begin_on_both_sides_of_a_part(dtype, heads, kv, dh, window):
+    """Parts are 512 slots of this handle; the chunk's first rows see one more of them than its last ones."""
+    print(f"case {dtype} {heads}/{kv}x{dh} window {window}", flush=True)
+    c = Call([(6, 512 * j + window - 4) for j in (1, 2, 3)] + [(8, 1024 + window - 8)], heads, kv, dh, dtype, max_ctx=6000, seed=window)
+    q = c.randn((c.rows, heads * dh), scale=2.0)
+    got = assert_rows_alone(c, q, window, torch.float32)
+    assert_within(got, *c.expected(q, window=window, u_out=2.0 ** -24))
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dh", HEADS)
+def test_masks_of_a_chain(dtype, heads, kv, dh):
+    """Rows whose mask allows their own and the earlier ones, beside branches that see less: the bits of a single token."""
+    most = 64 * kv // heads
+    print(f"case {dtype} {heads}/{kv}x{dh}", flush=True)
+    c = Call([(min(8, most), 1020), (most, 61), (min(5, most), 0)], heads, kv, dh, dtype, seed=11)
+    q = climbing(c, 2.0)
+    chain = torch.tensor([(2 << i) - 1 if i < 63 else -1 for n, _ in c.seqs for i in range(n)], dtype=torch.int64, device="cuda")
+    mask = chain.clone()
+    branch = torch.tensor([i for b, (n, _) in enumerate(c.seqs) for i in range(c.start[b], c.start[b] + n) if (i - c.start[b]) % 3 == 2],
+                          device="cuda")
+    mask[branch] &= 0x5555555555555555
+    got = c.attend(q, mask=mask)
+    assert_within(got, *c.expected(q, mask=mask))
+    for b, (n, _) in enumerate(c.seqs):
+        for i in range(n):
+            if mask[c.start[b] + i] == chain[c.start[b] + i]:
+                same = torch.equal(got[c.start[b] + i], alone(c, b, i, q))
+                assert same, f"row {i} of sequence {b}"
