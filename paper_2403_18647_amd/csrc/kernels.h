@@ -221,6 +221,12 @@ constexpr int kPagedMaxPairs = 1 << 19;  // sequences and key heads of a call (a
 constexpr int kPagedMaxParts = 64;       // parts of a short chunk, at most
 constexpr int kPagedMaxTileParts = 16;   // parts of a tile, at most
 constexpr int kPagedTileParts = 512;    // of all tiles and key heads, at most, where tiles have several
+// Parts of a tile's pages, where `tiles` of them (and key heads) leave compute units idle: more than one only where
+// tiles * Hkv * parts <= kPagedTileParts, which is what the scratch holds, whatever tiles the call's numbers come to.
+constexpr int paged_tile_splits(int tiles, int Hkv) {
+    const long pairs = (long)tiles * Hkv, room = pairs > 0 ? kPagedTileParts / pairs : kPagedTileParts;
+    return room < 1 ? 1 : room > kPagedMaxTileParts ? kPagedMaxTileParts : (int)room;
+}
 struct PagedPlan {
     int part_shift, max_parts;           // of the handle
     int tile_wgs, few_wgs, call_parts;   // of a call: workgroups; parts of a short chunk, at most

@@ -40,10 +40,6 @@ namespace sdsat {
 
 static constexpr float kRaise = 8.f;
 
-// parts of a tile's pages, where `tiles` of them (and key heads) leave compute units idle; tiles * Hkv * splits <= kPagedTileParts
-__device__ __forceinline__ int tile_splits(int tiles, int Hkv) {
-    return max(1, min(kPagedMaxTileParts, kPagedTileParts / max(1, tiles * Hkv)));
-}
 static constexpr int kWaves = 4;
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
@@ -651,7 +647,7 @@ __device__ __forceinline__ TileWork tile_work(const PagedAttnArgs& a, int want, 
         return q.n * (long)group > kPagedFewRows ? (q.n * group + kPagedTileRows - 1) / kPagedTileRows : 0;
     };
     TileWork t{};
-    t.splits = tile_splits(count_pieces(a.seq, lane, tiles_of), a.Hkv);
+    t.splits = paged_tile_splits(count_pieces(a.seq, lane, tiles_of), a.Hkv);
     const int each = by_slot ? 1 : t.splits;
     const Found f = find_piece(a.seq, want, lane, [&](const PagedSeq& q) { return tiles_of(q) * each * a.Hkv; });
     if (!f.ok) return t;
