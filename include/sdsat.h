@@ -390,7 +390,9 @@ int sdsat_paged_append(sdsat_paged* paged, const sdsat_paged_batch* batch, void*
  * them (s among them).  With d_mask ([rows] uint64, max_q <= 64, no window) it sees the slots below
  * d_len and of its chunk's rows j those with bit j set.  A row that sees nothing gives zeros.
  * scale 0: 1 / sqrt(head_dim).  d_out: [rows, ld_out], the pool's type or fp32.  Scores, sums and
- * outputs are accumulated in float; the weights are rounded to the pool's type.  While a chunk has
+ * outputs are accumulated in float.  The weights of a bf16 pool count with 16 bits (float accuracy); chunks
+ * of more than 64 rows * n_heads / n_kv_heads with outputs in bf16 round them to that type, in two thirds
+ * of the time that float outputs of such chunks take.  While a chunk has
  * rows * n_heads / n_kv_heads <= 64, its rows' results depend, for one handle configuration, neither on
  * the rest of the call nor on the chunk's length: a token decoded alone and the same token in a draft
  * block give the same bits.  Longer chunks are summed in an order that the call's number of rows

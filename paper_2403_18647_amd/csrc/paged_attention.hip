@@ -8,8 +8,11 @@
 //
 // The scores of 32 slots and 32 packed rows are formed as S^T = K Q^T, so that a lane has 16 slots of one row (its row's
 // others are in lane ^ 32), and enter O^T += V^T P^T as they stand: K's rows are read in the order in which V's pages hold
-// their slots.  P is rounded to the cache's type (half a step of bf16, 2^-8 of each weight at the most, on the way to an output that
-// is rounded as coarsely; the row's sum takes the unrounded weights); scores, sums and O are float.  A row keeps a base,
+// their slots.  Scores, sums and O are float.  On bf16 pools P enters as value and remainder (16 bits), which costs nothing
+// where memory is waited for (a token each of 64 sequences 143 and 144 us) and half the time again where the matrix cores
+// are (4096 rows behind 4096 slots 438 and 648 us): there, in tiles, P is rounded to bf16 where the output is too (half a
+// step, 2^-8 of each weight at the most, on the way to an output that is rounded as coarsely; the row's sum takes the
+// unrounded weights), and enters whole where the output is float.  A row keeps a base,
 // in units of log 2, that its weights are 2 to the score above; the base is raised, and O scaled, only when a score passes
 // it by more than kRaise: in most blocks nothing is scaled.
 //
@@ -109,12 +112,16 @@ struct Fetch {
     }
     template <int N, int AUX, int I = 0>   // pieces first .. first + N - 1 (first a multiple of VARS), to their places
     __device__ __forceinline__ void pieces(const unsigned char* src, unsigned char* dst, int first) const {
+#ifdef __HIP_DEVICE_COMPILE__   // the host's pass over several kernels that load alike does not know the builtin
         if constexpr (I < N) {
             const int at = (first + I / 4 * 4) * 1024;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_rsrc(src, P::HALF), (__attribute__((address_space(3))) void*)(dst + at), 16,
                                                      off[I % VARS], at, I % 4 * 1024, AUX);
             pieces<N, AUX, I + 1>(src, dst, first);
         }
+#else
+        (void)src, (void)dst, (void)first;
+#endif
     }
 };
 // Eight fragments out of LDS, and the wait for them.  In one piece of assembly: the compiler holds every read of LDS behind
@@ -238,23 +245,43 @@ __device__ __forceinline__ Frag<T> select_values(Frag<T> f, int want) {
     }
     return Frag<T>::from_f32(x);
 }
-__device__ __forceinline__ bool not_finite(const Frag<uint16_t>& f) {   // all ones in an exponent
-    bool b = false;
+// a value's sign bit set in `seen` where an exponent is all ones: one more there carries into it
+__device__ __forceinline__ void mark_not_finite(const Frag<uint16_t>& f, uint32_t& seen) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b |= ((f.v[j] & 0x7F80u) == 0x7F80u) | ((f.v[j] & 0x7F800000u) == 0x7F800000u);
-    return b;
+    for (int j = 0; j < 4; ++j) seen |= (f.v[j] & 0x7F807F80u) + 0x00800080u;
 }
-__device__ __forceinline__ bool not_finite(const Frag<float>& f) {
-    bool b = false;
+__device__ __forceinline__ void mark_not_finite(const Frag<float>& f, uint32_t& seen) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) b |= !(fabsf(f.get(j)) < INFINITY);
-    return b;
+    for (int j = 0; j < 8; ++j) seen |= (__float_as_uint(f.get(j)) & 0x7F800000u) + 0x00800000u;
 }
+template <typename T>
+constexpr uint32_t kSignBits = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+
+// The weights of a page, as the second product takes them.  FINE, bf16 pools: as value and remainder (16 bits of each), so
+// that they are no rounding point.
+template <typename T, bool FINE>
+struct Weights {
+    static constexpr bool REST = FINE && sizeof(T) == 2;
+    Frag<T> p[2], rest[REST ? 2 : 1];
+    __device__ __forceinline__ void set(const float (&w)[16]) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            p[s] = Frag<T>::from_f32(w + 8 * s);
+            if constexpr (REST) {
+                float r[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) r[j] = w[8 * s + j] - p[s].get(j);
+                rest[s] = Frag<T>::from_f32(r);
+            }
+        }
+    }
+};
 
 // A wave's 32 rows: queries, and the running softmax over NB pages at a time.
-template <typename T, int DH, int NB>
+template <typename T, int DH, int NB, bool FINE>
 struct RowWave {
     static constexpr int KS = DH / 16, DT = DH / 32;
+    using W = Weights<T, FINE>;
     Frag<T> q[KS];
     f32x16_t o[DT];
     float base, sum;   // base -inf: nothing seen yet
@@ -287,7 +314,7 @@ struct RowWave {
         for (int ks = 0; ks < KS; ++ks) mma32(s, k[ks], q[ks]);
     }
     // scores of pages blk .. to weights; masked: some row does not see all of them (pages from `end` on: none does)
-    __device__ __forceinline__ void weigh(const f32x16_t (&s)[NB], Frag<T> (&p)[NB][2], int blk, int end, bool masked, const Sight& see,
+    __device__ __forceinline__ void weigh(const f32x16_t (&s)[NB], W (&p)[NB], int blk, int end, bool masked, const Sight& see,
                                           float scale, int lane) {
         float x[NB][16];
 #pragma unroll
@@ -333,21 +360,22 @@ struct RowWave {
                 w[i] = __builtin_amdgcn_exp2f(fmaf(x[n][i], scale, minus));
                 sum += w[i];
             }
-            p[n][0] = Frag<T>::from_f32(w);
-            p[n][1] = Frag<T>::from_f32(w + 8);
+            p[n].set(w);
         }
     }
     // O += P V of one page.  Where a row does not see all of the page, values that are not finite must not reach it
     // through a weight of zero: they are taken out of the product, and infinities and NaN of slots that do count are put in
-    // by products with where they stand.
-    __device__ __forceinline__ void weighted(const Frag<T> (&p)[2], Frag<T> (&v)[KS], bool masked) {
+    // by products with where they stand.  Nor may such values meet remainders, which have either sign: a page that holds
+    // any is weighted without them.
+    __device__ __forceinline__ void weighted(const W& p, Frag<T> (&v)[KS], bool masked) {
         bool odd = false;
-        if (masked) {
+        if (W::REST || masked) {
+            uint32_t seen = 0;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) odd |= not_finite(v[i]);
-            odd = __any(odd);
+            for (int i = 0; i < KS; ++i) mark_not_finite(v[i], seen);
+            odd = __any((seen & kSignBits<T>) != 0);
         }
-        if (odd) {
+        if (masked && odd) {
             // one copy of this, on tile 0, the tiles taking turns there
 #pragma unroll 1
             for (int dt = 0; dt < DT; ++dt) {
@@ -357,7 +385,7 @@ struct RowWave {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) d[i] = 0.f;
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) mma32(d, select_values(v[s * DT], want), p[s]);
+                    for (int s = 0; s < 2; ++s) mma32(d, select_values(v[s * DT], want), p.p[s]);
                     const float x = want == 1 ? INFINITY : want == 2 ? -INFINITY : NAN;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[0][i] += d[i] > 0.f ? x : 0.f;
@@ -376,7 +404,13 @@ struct RowWave {
             }
         }
 #pragma unroll
-        for (int i = 0; i < KS; ++i) mma32(o[i % DT], v[i], p[i / DT]);
+        for (int i = 0; i < KS; ++i) mma32(o[i % DT], v[i], p.p[i / DT]);
+        if constexpr (W::REST) {
+            if (!odd) {
+#pragma unroll
+                for (int i = 0; i < KS; ++i) mma32(o[i % DT], v[i], p.rest[i / DT]);
+            }
+        }
     }
     __device__ __forceinline__ float whole_sum() const {
         const uint32_t u = __float_as_uint(sum);
@@ -510,7 +544,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
                                          unsigned char* smem, int wave, int lane) {
     using P = PageTile<T, DH>;
     constexpr int DT = DH / 32, QUADS = 4 * DT;
-    RowWave<T, DH, 1> w;
+    RowWave<T, DH, 1, true> w;
     w.clear();
     const Sight see = sight_of<T, DH>(a, r, 0, lane);
     const int begin = sp << a.part_shift;
@@ -544,7 +578,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
             const int blk = first + i * kWaves;
             const bool more = i + 1 < cnt, masked = 32 * blk + 31 > see.all_last || 32 * blk < see.all_first;
             f32x16_t s[1];
-            Frag<T> p[1][2];
+            Weights<T, true> p[1];
             wait_loads<P::PIECES>();   // K; V's are behind
             Frag<T> f[DH / 16];
             rd.template k<0>(f);
@@ -665,7 +699,7 @@ __device__ __forceinline__ TileWork tile_work(const PagedAttnArgs& a, int want, 
     return t;
 }
 
-template <typename T, int DH>
+template <typename T, int DH, bool FINE>
 __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsigned char* smem, int wave, int lane) {
     using P = PageTile<T, DH>;
     constexpr int DT = DH / 32, NL = P::PIECES / 2;   // 1 KiB loads of a wave per step, of K and of V
@@ -683,7 +717,7 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
         x.rows = min(32, r.rows - w0);
         page_range(a, x, wlo, whi);
     }
-    RowWave<T, DH, 2> w;
+    RowWave<T, DH, 2, FINE> w;
     w.clear();
     const size_t page_bytes = (size_t)a.Hkv * P::HALF;
     const unsigned char* kb = reinterpret_cast<const unsigned char*>(a.kp) + (size_t)h * P::HALF;
@@ -724,7 +758,8 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
         if (blk < whi && blk + 2 > wlo) {
             const bool masked = 32 * blk + 63 > see.all_last || 32 * blk < see.all_first || blk + 2 > hi;
             f32x16_t s[2];
-            Frag<T> p[2][2], f[DH / 16];
+            Weights<T, FINE> p[2];
+            Frag<T> f[DH / 16];
             rd.template k<0>(f);
             w.scores(s[0], f);
             rd.template k<P::BLK>(f);
@@ -853,7 +888,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a, int fe
 }
 
 // ------------------------------------------------------------------ the launch
-template <typename T, int DH, bool TILES>
+template <typename T, int DH, bool TILES, bool FINE>
 __global__ void __launch_bounds__(64 * kWaves, sizeof(T) * DH > 256 ? 1 : 2) paged_attn_kernel(PagedAttnArgs a) {
     __shared__ __align__(1024) unsigned char smem[kLdsBytes<T, DH>];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -861,7 +896,7 @@ __global__ void __launch_bounds__(64 * kWaves, sizeof(T) * DH > 256 ? 1 : 2) pag
     int few = (int)blockIdx.x;
     if constexpr (TILES) {
         if (few < a.tile_wgs) {
-            tile_rows<T, DH>(a, few, smem, wave, lane);
+            tile_rows<T, DH, FINE>(a, few, smem, wave, lane);
             return;
         }
         few -= a.tile_wgs;
@@ -910,10 +945,10 @@ size_t paged_part_floats(const PagedPlan& p, int H, int Hkv, int head_dim, int m
 template <typename T, int DH>
 static hipError_t launch_dh(const PagedPlan& p, const PagedAttnArgs& a, hipStream_t s) {
     const unsigned grid = (unsigned)p.tile_wgs + (unsigned)p.few_wgs;
-    if (p.tile_wgs)
-        hipLaunchKernelGGL((paged_attn_kernel<T, DH, true>), dim3(grid), dim3(64 * kWaves), 0, s, a);
-    else
-        hipLaunchKernelGGL((paged_attn_kernel<T, DH, false>), dim3(grid), dim3(64 * kWaves), 0, s, a);
+    auto kern = !p.tile_wgs ? paged_attn_kernel<T, DH, false, false>
+                : sizeof(T) == 2 && a.out_f32 ? paged_attn_kernel<T, DH, true, true>
+                                              : paged_attn_kernel<T, DH, true, false>;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * kWaves), 0, s, a);
     // tiles in several parts are kPagedTileParts / 2 at the most, with key heads
     const int subs = (long)a.seq.max_q * (a.H / a.Hkv) > 32 ? kPagedFewRows / 32 : 1, slices = p.call_parts > 8 ? 4 : 1;
     const int few = p.call_parts > 1 ? a.seq.B * a.Hkv * subs * slices : 0;
