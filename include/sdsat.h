@@ -388,7 +388,8 @@ int sdsat_paged_append(sdsat_paged* paged, const sdsat_paged_batch* batch, void*
 /* Attention of the new tokens' queries d_q ([rows, ld_q], the pool's type) over their sequences' pages,
  * which hold the new tokens too.  A row at slot s sees slots 0..s, with window > 0 the last `window` of
  * them (s among them).  With d_mask ([rows] uint64, max_q <= 64, no window) it sees the slots below
- * d_len and of its chunk's rows j those with bit j set.  A row that sees nothing gives zeros.
+ * d_len and of its chunk's rows j those with bit j set.  A row that sees nothing, or only
+ * scores of -inf, gives zeros.
  * scale 0: 1 / sqrt(head_dim).  d_out: [rows, ld_out], the pool's type or fp32.  Scores, sums and
  * outputs are accumulated in float.  The weights of a bf16 pool count with 16 bits (float accuracy); chunks
  * of more than 64 rows * n_heads / n_kv_heads with outputs in bf16 round them to that type, in two thirds

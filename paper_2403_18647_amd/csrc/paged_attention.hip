@@ -229,7 +229,7 @@ struct Sight {
     }
 };
 
-// finite values as they are, others as zero; want 0: that, 1: ones where +inf, 2: where -inf, 3: where NaN
+// want 0: finite values as they are, others as zero; ones where +inf (1), -inf (2), NaN (3), any of them (4)
 template <typename T>
 __device__ __forceinline__ Frag<T> select_values(Frag<T> f, int want) {
     // opaque: nothing of this is formed ahead for the steps that do not need it
@@ -240,7 +240,7 @@ __device__ __forceinline__ Frag<T> select_values(Frag<T> f, int want) {
     for (int j = 0; j < 8; ++j) {
         const float v = f.get(j);
         const bool nan = v != v, inf = !nan && fabsf(v) == INFINITY;
-        const bool hit = want == 1 ? inf && v > 0.f : want == 2 ? inf && v < 0.f : nan;
+        const bool hit = want == 1 ? inf && v > 0.f : want == 2 ? inf && v < 0.f : nan || (want == 4 && inf);
         x[j] = want == 0 ? (nan || inf ? 0.f : v) : hit ? 1.f : 0.f;
     }
     return Frag<T>::from_f32(x);
@@ -313,6 +313,10 @@ struct RowWave {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) mma32(s, k[ks], q[ks]);
     }
+    // the slot of a lane's i-th score of a page
+    __device__ __forceinline__ static int slot_of(int page, int i, int lane) {
+        return 32 * page + 16 * (i / 4 % 2) + 8 * (i / 8) + 4 * (lane >> 5) + i % 4;
+    }
     // scores of pages blk .. to weights; masked: some row does not see all of them (pages from `end` on: none does)
     __device__ __forceinline__ void weigh(const f32x16_t (&s)[NB], W (&p)[NB], int blk, int end, bool masked, const Sight& see,
                                           float scale, int lane) {
@@ -327,8 +331,7 @@ struct RowWave {
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int slot = 32 * (blk + n) + 16 * (i / 4 % 2) + 8 * (i / 8) + 4 * (lane >> 5) + i % 4;
-                    x[n][i] = ((blk + n < end) & see.sees(slot)) ? x[n][i] : -INFINITY;
+                    x[n][i] = ((blk + n < end) & see.sees(slot_of(blk + n, i, lane))) ? x[n][i] : -INFINITY;
                 }
         }
         float top = x[0][0];
@@ -363,29 +366,42 @@ struct RowWave {
             p[n].set(w);
         }
     }
-    // O += P V of one page.  Where a row does not see all of the page, values that are not finite must not reach it
-    // through a weight of zero: they are taken out of the product, and infinities and NaN of slots that do count are put in
-    // by products with where they stand.  Nor may such values meet remainders, which have either sign: a page that holds
-    // any is weighted without them.
-    __device__ __forceinline__ void weighted(const W& p, Frag<T> (&v)[KS], bool masked) {
+    // O += P V of page blk.  Values that are not finite must not meet weights of slots that a row does not see, which are
+    // zero, nor remainders, which have either sign: they are taken out of the product, and infinities and NaN of slots that
+    // do count are put in by products with where they stand (NaN where a slot is seen, but its weight is below the smallest
+    // float: zero times infinity).
+    __device__ __forceinline__ void weighted(const W& p, Frag<T> (&v)[KS], int blk, int end, bool masked, const Sight& see, int lane) {
         bool odd = false;
-        if (W::REST || masked) {
+        int fine = FINE;
+        asm volatile("" : "+s"(fine));   // a branch all the same: without it O and V are copied ahead of the rare part, into scratch
+        const bool look = masked || fine != 0;
+        if (look) {
             uint32_t seen = 0;
 #pragma unroll
             for (int i = 0; i < KS; ++i) mark_not_finite(v[i], seen);
             odd = __any((seen & kSignBits<T>) != 0);
         }
-        if (masked && odd) {
+        if (look && odd) {
+            asm volatile("" : "+v"(lane));
+            Frag<T> none[2];   // ones where a slot is seen with a weight of zero
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[j] = (!masked || (blk < end && see.sees(slot_of(blk, 8 * s + j, lane)))) && p.p[s].get(j) == 0.f ? 1.f : 0.f;
+                none[s] = Frag<T>::from_f32(x);
+            }
             // one copy of this, on tile 0, the tiles taking turns there
 #pragma unroll 1
             for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll 1
-                for (int want = 1; want < 4; ++want) {
+                for (int want = 1; want < 5; ++want) {
                     f32x16_t d;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) d[i] = 0.f;
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) mma32(d, select_values(v[s * DT], want), p.p[s]);
+                    for (int s = 0; s < 2; ++s) mma32(d, select_values(v[s * DT], want), want == 4 ? none[s] : p.p[s]);
                     const float x = want == 1 ? INFINITY : want == 2 ? -INFINITY : NAN;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[0][i] += d[i] > 0.f ? x : 0.f;
@@ -406,10 +422,8 @@ struct RowWave {
 #pragma unroll
         for (int i = 0; i < KS; ++i) mma32(o[i % DT], v[i], p.p[i / DT]);
         if constexpr (W::REST) {
-            if (!odd) {
 #pragma unroll
-                for (int i = 0; i < KS; ++i) mma32(o[i % DT], v[i], p.rest[i / DT]);
-            }
+            for (int i = 0; i < KS; ++i) mma32(o[i % DT], v[i], p.rest[i / DT]);
         }
     }
     __device__ __forceinline__ float whole_sum() const {
@@ -595,7 +609,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnArgs& a, const Rows& r, 
             rd.template v<0>(f);
             if constexpr (sizeof(T) == 4) wait_lds();
             if (more) fv.template pieces<P::PIECES, 2>(vb + (size_t)id * page_bytes, s_v, 0);
-            w.weighted(p[0], f, masked);
+            w.weighted(p[0], f, blk, to, masked, see, lane);
         }
         if (bad) atomicOr(a.seq.err, 1);
     }
@@ -766,9 +780,9 @@ __device__ __forceinline__ void tile_rows(const PagedAttnArgs& a, int wg, unsign
             w.scores(s[1], f);
             w.weigh(s, p, blk, hi, masked, see, a.scale, lane);
             rd.template v<0>(f);
-            w.weighted(p[0], f, masked);
+            w.weighted(p[0], f, blk, hi, masked, see, lane);
             rd.template v<P::BLK>(f);
-            w.weighted(p[1], f, masked);
+            w.weighted(p[1], f, blk + 1, hi, masked, see, lane);
         }
         rd.move(i & 1 ? -2 * P::BLK : 2 * P::BLK);
     }
@@ -945,9 +959,10 @@ size_t paged_part_floats(const PagedPlan& p, int H, int Hkv, int head_dim, int m
 template <typename T, int DH>
 static hipError_t launch_dh(const PagedPlan& p, const PagedAttnArgs& a, hipStream_t s) {
     const unsigned grid = (unsigned)p.tile_wgs + (unsigned)p.few_wgs;
-    auto kern = !p.tile_wgs ? paged_attn_kernel<T, DH, false, false>
-                : sizeof(T) == 2 && a.out_f32 ? paged_attn_kernel<T, DH, true, true>
-                                              : paged_attn_kernel<T, DH, true, false>;
+    auto kern = p.tile_wgs ? paged_attn_kernel<T, DH, true, false> : paged_attn_kernel<T, DH, false, false>;
+    if constexpr (sizeof(T) == 2) {
+        if (p.tile_wgs && a.out_f32) kern = paged_attn_kernel<T, DH, true, true>;
+    }
     hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * kWaves), 0, s, a);
     // tiles in several parts are kPagedTileParts / 2 at the most, with key heads
     const int subs = (long)a.seq.max_q * (a.H / a.Hkv) > 32 ? kPagedFewRows / 32 : 1, slices = p.call_parts > 8 ? 4 : 1;

@@ -6,7 +6,7 @@ from paper_2403_18647_amd import binding as B
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from paged_helpers import Call, assert_within   # noqa: E402
+from paged_helpers import Call, assert_within, place   # noqa: E402
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -102,3 +102,30 @@ def test_masks_of_a_chain(dtype, heads, kv, dh):
             if mask[c.start[b] + i] == chain[c.start[b] + i]:
                 same = torch.equal(got[c.start[b] + i], alone(c, b, i, q))
                 assert same, f"row {i} of sequence {b}"
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dtype,heads,kv,dh", HEADS)
+def test_values_that_are_not_finite_with_weights_of_zero(dtype, heads, kv, dh, value):
+    """A slot whose weight is below the smallest float and whose value is not finite makes NaN of the rows that see it, in a
+    page that the chunk sees in part as in one that a single token sees whole; rows ahead of it do not meet it."""
+    print(f"case {dtype} {heads}/{kv}x{dh} {value}", flush=True)
+    n, cached, at = 6, 60, 61
+    c = Call([(n, cached)], heads, kv, dh, dtype, seed=5)
+    q = c.randn((c.rows, heads * dh)).abs() + 1
+    page, slot = c.slots(0, at, at + 1)
+    c.k[page, :, slot] = -40.0   # scores of -40 sqrt(dh) and less
+    for out_type in (None, torch.float32):
+        before = c.attend(q, out=torch.zeros_like(q, dtype=out_type or q.dtype))
+        keep = c.v.clone()
+        c.v[page, 0, 7, place(at)] = value
+        got = c.attend(q, out=torch.zeros_like(before))
+        hit = torch.zeros((n, heads, dh), dtype=torch.bool, device="cuda")
+        hit[at - cached:, :heads // kv, 7] = True
+        assert torch.equal(got.isnan(), hit.view(n, -1))
+        assert torch.equal(got[~hit.view(n, -1)], before[~hit.view(n, -1)])
+        for i in range(n):
+            one = alone(c, 0, i, q, out_type=out_type)
+            same = torch.equal(one.nan_to_num(7.0), got[i].nan_to_num(7.0)) and torch.equal(one.isnan(), got[i].isnan())
+            assert same, f"row {i}"
+        c.v.copy_(keep)
