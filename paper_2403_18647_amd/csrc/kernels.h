@@ -211,6 +211,8 @@ struct PagedAppendArgs {
     int H, Hkv, interleaved, rot;
     double turns[kMaxPairs];
 };
+// a call without new tokens: its sequences' numbers are looked at all the same
+hipError_t launch_paged_check(const PagedSeqs& seq, hipStream_t s);
 hipError_t launch_paged_append(int dtype, int x_dtype, int head_dim, const PagedAppendArgs& a, hipStream_t s);
 
 // Attention.  Rows of the H / Hkv query heads that share a key head are packed, row i * group + head.  Sequences of up to

@@ -188,7 +188,7 @@ int sdsat_paged_append(sdsat_paged* p, const sdsat_paged_batch* batch, void* d_k
         a.mscale = rope->mscale;
         std::memcpy(a.turns, rope->turns, sizeof(a.turns));
     }
-    if (!batch->max_q) return SDSAT_OK;
+    if (!batch->max_q) return launched(p, launch_paged_check(a.seq, p->stream), "paged append");
     a.kp = d_k; a.vp = d_v; a.x = d_x; a.ldx = ld_x; a.qout = d_q; a.ldq = ld_q;
     a.pos = d_pos; a.q_gain = d_q_gain; a.k_gain = d_k_gain; a.eps = eps;
     a.H = c.n_heads; a.Hkv = c.n_kv_heads;
@@ -217,7 +217,7 @@ int sdsat_paged_attention(sdsat_paged* p, const sdsat_paged_batch* batch, const 
     if (scale == 0.f) scale = (float)(1.0 / std::sqrt((double)c.head_dim));
     const float in2 = scale * 1.44269504f;   // log2 e
     if (!(in2 > 0.f) || !std::isfinite(in2)) return fail(p, SDSAT_EINVAL, "scale must be positive and finite (0: 1 / sqrt(head_dim))");
-    if (!batch->max_q) return SDSAT_OK;
+    if (!batch->max_q) return launched(p, launch_paged_check(a.seq, p->stream), "paged attention");
     PagedPlan plan = p->plan;
     plan_paged_call(plan, c.n_heads, c.n_kv_heads, batch->batch, batch->rows, batch->max_q, batch->max_len);
     a.kp = d_k; a.vp = d_v; a.q = d_q; a.ldq = ld_q; a.mask = d_mask; a.out = d_out; a.ldo = ld_out;

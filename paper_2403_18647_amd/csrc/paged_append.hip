@@ -272,6 +272,14 @@ static hipError_t launch_append_dh(int head_dim, const PagedAppendArgs& a, hipSt
     return hipGetLastError();
 }
 
+__global__ void __launch_bounds__(64) paged_check_kernel(PagedSeqs seq) { check_seqs(seq, threadIdx.x); }
+
+hipError_t launch_paged_check(const PagedSeqs& q, hipStream_t s) {
+    if (q.B < 1 || !q.start || !q.len || !q.err) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(paged_check_kernel, dim3(1), dim3(64), 0, s, q);
+    return hipGetLastError();
+}
+
 hipError_t launch_paged_append(int dtype, int x_dtype, int head_dim, const PagedAppendArgs& a, hipStream_t s) {
     const PagedSeqs& q = a.seq;
     if ((head_dim != 64 && head_dim != 128) || q.B < 1 || q.rows < 0 || q.pages_ld < 1 || q.n_pages < 1 || q.max_q < 0 ||

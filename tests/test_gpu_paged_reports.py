@@ -44,3 +44,54 @@ def test_starts_that_go_back_and_forth(n, count):
     c.batch = B.paged_batch(c.d_start, c.d_len, c.pages, rows, n, n + 40)
     assert_within(c.attend(q), want, tol)
     B.sdsat_paged_status(c.handle)
+
+
+@pytest.mark.parametrize("call", ["append", "attention"])
+@pytest.mark.parametrize("batch", [1, 3, 200])
+def test_calls_without_new_tokens_look_at_their_sequences(call, batch):
+    """The host says that no sequence has new tokens: one that does, or whose numbers do not fit otherwise, is reported; and
+    nothing is written."""
+    print(f"case {call} {batch}", flush=True)
+    c = Call([(0, 40)] * batch, 4, 2, 64, spare=5)
+    x = c.randn((c.rows, 512))
+    q = torch.full((c.rows, 256), 3.0, dtype=c.dtype, device="cuda")
+    k, v = c.k.clone(), c.v.clone()
+
+    def run():
+        if call == "append":
+            B.sdsat_paged_append(c.handle, c.batch, c.k, c.v, x, q_out=q)
+        else:
+            B.sdsat_paged_attention(c.handle, c.batch, c.k, c.v, q.clone(), out=q)
+        assert (q == 3).all() and torch.equal(c.k, k) and torch.equal(c.v, v)
+
+    assert c.max_q == 0
+    run()
+    B.sdsat_paged_status(c.handle)
+    for t, at, value in ((c.d_start, batch, 2), (c.d_start, 0, -1), (c.d_len, batch - 1, -1), (c.d_len, batch // 2, 41)):
+        keep = t.clone()
+        t[at] = value
+        run()
+        assert_reported(c)
+        t.copy_(keep)
+        run()
+        B.sdsat_paged_status(c.handle)
+
+
+def test_a_captured_call_without_new_tokens():
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        c = Call([(0, 40), (0, 7)], 4, 2, 64, spare=2)
+        q = torch.full((c.rows, 256), 3.0, dtype=c.dtype, device="cuda")
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            c.attend(q, out=q)
+        for start, bad in ((0, False), (1, True), (0, False)):
+            c.d_start[2] = start
+            graph.replay()
+            stream.synchronize()
+            assert (q == 3).all()
+            if bad:
+                assert_reported(c)
+            else:
+                B.sdsat_paged_status(c.handle)
