@@ -55,6 +55,7 @@ class sdsat_paged_batch(ctypes.Structure):
     _fields_ = [("d_start", ctypes.c_void_p), ("d_len", ctypes.c_void_p), ("d_pages", ctypes.c_void_p),
                 ("batch", ctypes.c_int32), ("pages_ld", ctypes.c_int32), ("rows", ctypes.c_int32),
                 ("max_q", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+    device = None   # index of its tensors', where paged_batch() made it
 
 
 class sdsat_rope(ctypes.Structure):
@@ -238,6 +239,9 @@ def logit_rules(history=None, history_len=None, prompt_len=None, tokens=None, ma
     and prompt_len [batch], tokens [batch, q]; int64 mask [batch * q]; float32 penalties [3, batch] (repetition, frequency,
     presence) and bias [V], [1, V] or [batch, V]; int32 allowed [batch * q, words], a bit for each id."""
     _dense(history, history_len, prompt_len, tokens, mask, penalties, bias, allowed)
+    _elements("int32", history=history, history_len=history_len, prompt_len=prompt_len, tokens=tokens, allowed=allowed)
+    _elements("int64", mask=mask)
+    _elements("float32", penalties=penalties, bias=bias)
     shared = bias is None or bias.dim() == 1 or bias.shape[0] == 1
     r = sdsat_logit_rules(_ptr(history), _ptr(history_len), _ptr(prompt_len), 0 if history is None else history.shape[-1],
                           _ptr(tokens), _ptr(mask), _ptr(penalties), _ptr(bias), 0 if shared else bias.shape[-1],
@@ -247,6 +251,9 @@ def logit_rules(history=None, history_len=None, prompt_len=None, tokens=None, ma
 
 
 def sdsat_adjust_logits(ctx, batch, q, logits, rules, out):
+    for t in (logits, out):
+        if not isinstance(t, int) and (str(t.dtype) != "torch.float32" or not t.is_contiguous()):
+            raise ValueError("logits and out must be float32 and contiguous")
     _check(lib().sdsat_adjust_logits(ctx, batch, q, _ptr(logits), ctypes.byref(rules), _ptr(out)), ctx)
 
 
@@ -256,19 +263,112 @@ def _dense(*tensors):
             raise ValueError("tensor must be contiguous")
 
 
-def _dtype_code(t):
+def _elements(kind, **tensors):
+    """Tensors (None, addresses: not looked at) hold elements of this type; for int32 and int64 the unsigned one does too."""
     import torch
-    codes = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+    allowed = [getattr(torch, n) for n in (kind, "u" + kind) if hasattr(torch, n)]
+    for name, t in tensors.items():
+        if t is not None and not isinstance(t, int) and t.dtype not in allowed:
+            raise ValueError(f"{name} must be {kind}, not {t.dtype}")
+
+
+def _dtype_codes():
+    import torch
+    return {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+
+
+def _dtype_code(t):
+    codes = _dtype_codes()
     if t.dtype not in codes:
         raise ValueError("tensor must be float32 or bfloat16")
     return codes[t.dtype]
 
 
-def _row_stride(t, columns=None):
-    """Elements between rows of a 2-D tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+def _row_stride(t, rows=0, columns=0):
+    """Elements between rows of a 2-D tensor whose rows are contiguous, at least `rows` of at least `columns`."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("tensor must be 2-D with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    n, width = shape
+    if n < rows or width < columns:
+        raise ValueError(f"tensor of {n} rows of {width} elements, fewer than the call's {rows} rows of {columns}")
+    return stride[0] if n > 1 else max(stride[0], width)
+
+
+class _PagedLimits:
+    """What a handle's tensors have to be like, kept beside it: looked at in every call, for a microsecond of the host's
+    time (the library sees addresses only)."""
+
+    def __init__(self, cfg, workspace):
+        import torch
+        self.dtype = torch.bfloat16 if cfg.dtype == DTYPE_BF16 else torch.float32
+        self.k_shape = torch.Size((cfg.n_pages, cfg.n_kv_heads, PAGE, cfg.head_dim))
+        self.v_shape = torch.Size((cfg.n_pages, cfg.n_kv_heads, cfg.head_dim, PAGE))
+        self.q_columns = cfg.n_heads * cfg.head_dim
+        self.x_columns = (cfg.n_heads + 2 * cfg.n_kv_heads) * cfg.head_dim
+        self.head_dim, self.max_rows = cfg.head_dim, cfg.max_rows
+        self.device = workspace.get_device()
+        self.codes = _dtype_codes()
+        self.pool_codes = {self.dtype: cfg.dtype}
+        self.float32, self.int32, self.int64 = ((d,) for d in (torch.float32, torch.int32, torch.int64))
+        if hasattr(torch, "uint32"):
+            self.int32, self.int64 = (torch.int32, torch.uint32), (torch.int64, torch.uint64)
+
+    def elsewhere(self, t, what):
+        if t.is_cuda or not t.is_pinned():
+            raise ValueError(f"{what} is on another device than the handle")
+
+    def rows(self, batch):
+        """A call's rows, as far as tensors must have them: the library refuses calls of more than it takes."""
+        if batch.device != self.device and batch.device is not None:
+            raise ValueError("the batch's tensors are on another device than the handle")
+        return batch.rows if batch.rows <= self.max_rows else 0
+
+    def pools(self, k, v):
+        """Addresses of K and V."""
+        try:
+            if (k.shape == self.k_shape and v.shape == self.v_shape and k.dtype is self.dtype and v.dtype is self.dtype and
+                    k.get_device() == self.device and v.get_device() == self.device and k.is_contiguous() and v.is_contiguous()):
+                return k.data_ptr(), v.data_ptr()
+        except AttributeError:   # addresses
+            pass
+        return self.pool(k, self.k_shape, "k"), self.pool(v, self.v_shape, "v")
+
+    def pool(self, t, shape, what):
+        if t is None or isinstance(t, int):
+            return t
+        if t.shape != shape and (t.dim() != 4 or t.shape[1:] != shape[1:] or t.shape[0] < shape[0]):
+            raise ValueError(f"{what} must be {list(shape)}, not {list(t.shape)}")
+        if t.dtype is not self.dtype or not t.is_contiguous():
+            raise ValueError(f"{what} must be {self.dtype} and contiguous")
+        if t.get_device() != self.device:
+            self.elsewhere(t, what)
+        return t.data_ptr()
+
+    def rows_of(self, t, rows, columns, codes, what):
+        """Address, type and row stride of a call's rows."""
+        if t is None:
+            raise ValueError(f"{what} is missing")
+        code = codes.get(t.dtype)
+        if code is None:
+            raise ValueError(f"{what} must be {' or '.join(map(str, codes))}")
+        shape = t.shape
+        if len(shape) == 2 and t.is_contiguous() and shape[0] >= rows and shape[1] >= columns:
+            ld = shape[1]
+        else:
+            ld = _row_stride(t, rows, columns)
+        if t.get_device() != self.device:
+            self.elsewhere(t, what)
+        return t.data_ptr(), code, ld
+
+    def vector(self, t, kinds, n, what):
+        if isinstance(t, int):
+            return t
+        if t.dtype not in kinds or t.numel() < n or not t.is_contiguous():
+            raise ValueError(f"{what} must be at least {n} elements of {kinds[0]}, contiguous")
+        if t.get_device() != self.device:
+            self.elsewhere(t, what)
+        return t.data_ptr()
 
 
 def paged_batch(start, length, pages, rows, max_q, max_len) -> sdsat_paged_batch:
@@ -276,10 +376,16 @@ def paged_batch(start, length, pages, rows, max_q, max_len) -> sdsat_paged_batch
     length [batch], pages [batch, width]; rows of the call's arrays; host bounds of the new tokens of a sequence and of
     its slots with them."""
     _dense(start, length)
+    _elements("int32", start=start, length=length, pages=pages)
     if start.numel() != length.numel() + 1 or pages.dim() != 2 or pages.shape[0] != length.numel():
         raise ValueError("start must be [batch + 1], length [batch] and pages [batch, width]")
     b = sdsat_paged_batch(_ptr(start), _ptr(length), _ptr(pages), length.numel(), _row_stride(pages), rows, max_q, max_len)
+    if b.pages_ld > pages.shape[1] and max_len > PAGE * pages.shape[1]:
+        raise ValueError(f"max_len of {max_len} slots, {pages.shape[1]} pages of 32 in a row of the view")
     b.tensors = (start, length, pages)
+    b.device = start.get_device()
+    if length.get_device() != b.device or pages.get_device() != b.device:
+        raise ValueError("start, length and pages must be on one device")
     return b
 
 
@@ -308,23 +414,37 @@ def sdsat_paged_query_sizes(cfg: sdsat_paged_config) -> int:
 def sdsat_paged_init(cfg, workspace, stream=None):
     out = ctypes.c_void_p()
     _check(lib().sdsat_paged_init(ctypes.byref(cfg), _ptr(workspace), workspace.numel(), _stream(stream), ctypes.byref(out)))
+    out.limits = _PagedLimits(cfg, workspace)
     return out
 
 
 def sdsat_paged_append(paged, batch, k, v, x, rope=None, pos=None, q_gain=None, k_gain=None, eps=0.0, q_out=None):
-    """x [rows, (heads + 2 kv_heads) * head_dim] float32 or bfloat16, q_out [rows, heads * head_dim]; rows may be strided."""
-    _dense(k, v, pos, q_gain, k_gain)
-    _check_paged(lib().sdsat_paged_append(paged, ctypes.byref(batch), _ptr(k), _ptr(v), _ptr(x), _dtype_code(x),
-                                          _row_stride(x), None if rope is None else ctypes.byref(rope), _ptr(pos),
-                                          _ptr(q_gain), _ptr(k_gain), eps, _ptr(q_out), _row_stride(q_out)), paged)
+    """x [rows, (heads + 2 kv_heads) * head_dim] float32 or bfloat16, q_out [rows, heads * head_dim] in the pool's type; rows
+    may be strided.  k and v as Paged.pool() makes them, pos int32 [rows], gains float32 [head_dim]."""
+    t = paged.limits
+    rows = t.rows(batch)
+    k_at, v_at = t.pools(k, v)
+    x_at, x_code, x_ld = t.rows_of(x, rows, t.x_columns, t.codes, "x")
+    q_at, _, q_ld = t.rows_of(q_out, rows, t.q_columns, t.pool_codes, "q_out")
+    _check_paged(lib().sdsat_paged_append(paged, ctypes.byref(batch), k_at, v_at, x_at, x_code, x_ld,
+                                          None if rope is None else ctypes.byref(rope),
+                                          None if pos is None else t.vector(pos, t.int32, rows, "pos"),
+                                          None if q_gain is None else t.vector(q_gain, t.float32, t.head_dim, "q_gain"),
+                                          None if k_gain is None else t.vector(k_gain, t.float32, t.head_dim, "k_gain"),
+                                          eps, q_at, q_ld), paged)
 
 
 def sdsat_paged_attention(paged, batch, k, v, q, mask=None, window=0, scale=0.0, out=None):
-    """q [rows, heads * head_dim] in the pool's type, out the same or float32; rows may be strided."""
-    _dense(k, v, mask)
-    _check_paged(lib().sdsat_paged_attention(paged, ctypes.byref(batch), _ptr(k), _ptr(v), _ptr(q), _row_stride(q),
-                                             _ptr(mask), window, scale, _ptr(out), _dtype_code(out), _row_stride(out)),
-                 paged)
+    """q [rows, heads * head_dim] in the pool's type, out the same or float32; rows may be strided.  k and v as Paged.pool()
+    makes them, mask int64 [rows]."""
+    t = paged.limits
+    rows = t.rows(batch)
+    k_at, v_at = t.pools(k, v)
+    q_at, _, q_ld = t.rows_of(q, rows, t.q_columns, t.pool_codes, "q")
+    out_at, out_code, out_ld = t.rows_of(out, rows, t.q_columns, t.codes, "out")
+    _check_paged(lib().sdsat_paged_attention(paged, ctypes.byref(batch), k_at, v_at, q_at, q_ld,
+                                             None if mask is None else t.vector(mask, t.int64, rows, "mask"), window, scale,
+                                             out_at, out_code, out_ld), paged)
 
 
 def sdsat_paged_status(paged):
