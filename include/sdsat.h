@@ -368,7 +368,11 @@ int sdsat_rope_init(int32_t layout, int32_t rot_dims, double base, int32_t scali
 
 /* A handle for calls on one stream, for all layers (of one shape).  Workspace: device memory of
  * sdsat_paged_query_sizes() bytes, 256-byte aligned, the caller's, for the handle's lifetime; calls
- * on one handle, captured ones too, must not overlap.  sdsat_paged_init is synchronous. */
+ * on one handle, captured ones too, must not overlap.  The workspace holds parts of short chunks' results,
+ * at most 64 of each sequence: max_batch * n_kv_heads * parts * 64 * (head_dim + 4) floats, 0.3 GB for 64
+ * sequences of 32768 slots with 8 key heads of 128, 1.1 GB for 64 of 131072, 4.5 GB for 256 of them.  Parts
+ * suit a full handle: few sequences at a time are faster on one made for few (a token over 8000 slots of
+ * 8 key heads 15 us on a handle of that size, 27 on one for 64 sequences).  sdsat_paged_init is synchronous. */
 int sdsat_paged_query_sizes(const sdsat_paged_config* cfg, size_t* workspace_bytes);
 int sdsat_paged_init(const sdsat_paged_config* cfg, void* workspace, size_t workspace_bytes,
                      void* hip_stream, sdsat_paged** out);
@@ -396,8 +400,8 @@ int sdsat_paged_append(sdsat_paged* paged, const sdsat_paged_batch* batch, void*
  * of the time that float outputs of such chunks take.  While a chunk has
  * rows * n_heads / n_kv_heads <= 64, its rows' results depend, for one handle configuration, neither on
  * the rest of the call nor on the chunk's length: a token decoded alone and the same token in a draft
- * block give the same bits.  Longer chunks are summed in an order that the call's number of rows
- * decides; the same call gives the same bits.  Stream-ordered. */
+ * block give the same bits.  Longer chunks are summed in an order that the lengths of the call's
+ * chunks decide; the same call gives the same bits.  Stream-ordered. */
 int sdsat_paged_attention(sdsat_paged* paged, const sdsat_paged_batch* batch, const void* d_k,
                           const void* d_v, const void* d_q, int64_t ld_q, const uint64_t* d_mask,
                           int32_t window, float scale, void* d_out, int32_t out_dtype, int64_t ld_out);

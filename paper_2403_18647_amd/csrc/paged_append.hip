@@ -14,8 +14,8 @@
 // in a page (32 slots beside each other for one column): pages of more than kScatterTokens new tokens are turned in LDS and
 // written 16 bytes at a time where all of a chunk's slots are new; fewer tokens are written element by element.
 // Bound by memory, and by latency for single tokens: 4 prompts of 2047 tokens, 48 heads of 128 in bf16 (201 MB) 54 us,
-// 3.7 TB/s (a large copy 4.9; without the norms 51, one head at a time 73); one token of 64 sequences 8.4 us, a block of 6
-// tokens of the tiny decoder 6.7 (a call cannot take less than the host's launch, 4.4).
+// 3.7 TB/s (a large copy 4.9; without the norms 51, one head at a time 73); one token of 64 sequences 7.8 us, a block
+// of 6 tokens of the tiny decoder 5.2 (called from Python 9.0 and 6.8: the host's time; a launch alone is 4.4).
 #include <algorithm>
 
 #include "paged_device.h"

@@ -8,13 +8,13 @@
 //
 // The scores of 32 slots and 32 packed rows are formed as S^T = K Q^T, so that a lane has 16 slots of one row (its row's
 // others are in lane ^ 32), and enter O^T += V^T P^T as they stand: K's rows are read in the order in which V's pages hold
-// their slots.  Scores, sums and O are float.  On bf16 pools P enters as value and remainder (16 bits), which costs nothing
-// where memory is waited for (a token each of 64 sequences 143 and 144 us) and half the time again where the matrix cores
-// are (4096 rows behind 4096 slots 438 and 648 us): there, in tiles, P is rounded to bf16 where the output is too (half a
-// step, 2^-8 of each weight at the most, on the way to an output that is rounded as coarsely; the row's sum takes the
-// unrounded weights), and enters whole where the output is float.  A row keeps a base,
-// in units of log 2, that its weights are 2 to the score above; the base is raised, and O scaled, only when a score passes
-// it by more than kRaise: in most blocks nothing is scaled.
+// their slots.  Scores, sums and O are float.  On bf16 pools P enters as value and remainder (16 bits), which costs short
+// chunks 0 to 3% (a token each of 64 sequences 143 and 144.5 us, 11 rows of 8 over 4000 slots 47.6 and 49.0) and tiles half
+// the time again (4096 rows behind 4096 slots 434 and 652 us).  So tiles round P to bf16 where the output is rounded to it
+// too (half a step, 2^-8 of each weight at the most; error 0.0023 of the output's size, 0.0017 being its own rounding; the
+// row's sum takes the unrounded weights) and take it whole where the output is float.
+// A row keeps a base, in units of log 2, that its weights are 2 to the score above; the base is raised, and O scaled, only
+// when a score of the row's own passes it by more than kRaise: in most blocks nothing is scaled.
 //
 // Two kinds of workgroup of four waves, in one launch:
 //  * tiles, of chunks of more than kPagedFewRows packed rows: 128 rows, 32 for each wave; two pages at a time go straight
@@ -24,16 +24,17 @@
 //    the next scores are formed; no barriers.  The waves' results are joined by log-sum-exp in wave order.
 // A short chunk's part is 2^part_shift pages from a slot that is a multiple of them, the same for the handle's every call:
 // a row's result depends neither on what else is in its call nor on the chunk's other rows.  Tiles are in as many parts as
-// the call's number of them leaves room for, so that their results depend on it in the order of summation.  Results of parts go to scratch; a second launch joins them (in the workgroup that comes last it took longer:
-// 11 rows of 8 sequences over 3000 slots 47 us, 39 so).
+// the call's number of them leaves room for, so that their results depend on the call's chunks in the order of summation.
+// Results of parts go to scratch; a second launch joins them (in the workgroup that comes last it took longer: 11 rows of 8
+// sequences over 3000 slots 47 us, 39 so).
 //
 // Bound by memory where rows are few: a token each of 64 sequences of up to 4000 slots, 8 key heads of 128 in bf16 (893 MB),
-// 143 us, 6.2 TB/s; of one of 130000 (533 MB) 87, 6.1; and by the way to the first page and the second launch where slots
-// are few too (11 rows each of 4 sequences of 1500, 98 MB: 26 us, 14 at the rate of a read stream).  Long chunks are bound
-// by the matrix cores at the clock that the card holds under them: 4096 rows behind 4096 slots, 32 heads, 412 GFLOP, 423 us,
-// 975 TFLOP/s (a large product 1180 to 1230); the matrix pipes are busy 49% of the cycles, and without the softmax, or
-// without loads and barriers, it took about a tenth less.  A chunk of 1001 rows beside 31 single tokens: 166 us, 74 at
-// both rates.
+// 144 us, 6.2 TB/s; of one of 130000 (533 MB) 88, 6.1; and by the way to the first page and the second launch where slots
+// are few too (11 rows each of 4 sequences of 1500, 98 MB: 26 us, 14 at the rate of a read stream).  Long chunks keep
+// neither pipe full: 4096 rows behind 4096 slots, 32 heads, 412 GFLOP, take 417 to 435 us, 950 to 990 TFLOP/s (a large
+// product 1180 to 1230), with the vector pipes busy 58% of the cycles, for the softmax, and the matrix pipes 49%, at the
+// clock of 1.7 GHz that the card holds under both; without the softmax, or without loads and barriers, it took about a
+// tenth less.  A chunk of 1001 rows beside 31 single tokens: 165 us, 74 at both rates.
 #include <algorithm>
 #include <type_traits>
 
@@ -200,7 +201,7 @@ struct PageRead<uint16_t, DH> {
     }
 };
 
-// at most N loads are outstanding; what was read from LDS has arrived
+// at most N loads are outstanding
 template <int N>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("" ::: "memory");
@@ -925,7 +926,10 @@ PagedPlan plan_paged(int Hkv, int max_batch, int max_ctx) {
     // pages of a part: a full cache in about 1024 parts, four for each wave at the least.  us with 4, 8 and 16 at the least: a
     // token over 1500 slots of 8 key heads 15.1, 14.1, 15.1; 6 tokens of 4 sequences over 3000 37, 26, 20; 64 tokens over 500
     // slots 39, 39, 26; 11 rows of 4 sequences over 1500 slots of 32 heads 33, 31, 28.  512 to 4096 parts, 64 tokens over 4000
-    // slots: 167, 167, 173, 181.
+    // slots: 167, 167, 173, 181.  (All on handles of the call's own size.  Parts follow the handle, so that a row's bits do
+    // not follow the batch, and a handle for more has longer ones: one for 64 sequences of 16384 slots and more takes a token
+    // over 2000, 8000 and 16000 slots of 8 key heads in 23.5, 26.9 and 28.4 us, one of the call's size in 14.3, 14.7 and 16.9;
+    // 6 rows of 4 sequences over 3000 slots in 30, 19.4.)
     // (A power of two, as the kernels shift, near the number, and enough of them for a full cache in kPagedMaxParts.)
     const long want = std::min<long>((cap * pairs + 1023) / 1024, 64), least = (cap + kPagedMaxParts - 1) / kPagedMaxParts;
     p.part_shift = 4;
