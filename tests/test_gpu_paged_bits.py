@@ -129,3 +129,18 @@ def test_values_that_are_not_finite_with_weights_of_zero(dtype, heads, kv, dh, v
             same = torch.equal(one.nan_to_num(7.0), got[i].nan_to_num(7.0)) and torch.equal(one.isnan(), got[i].isnan())
             assert same, f"row {i}"
         c.v.copy_(keep)
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dh", HEADS)
+@pytest.mark.parametrize("out_type", [None, torch.float32])
+def test_rows_beside_a_long_chunk(dtype, heads, kv, dh, out_type):
+    """Short chunks in a call with tiles, with outputs in either type: the bits of a single token."""
+    print(f"case {dtype} {heads}/{kv}x{dh} {out_type}", flush=True)
+    c = Call([(5, 700), (300, 50), (1, 2200), (6, 29)], heads, kv, dh, dtype, seed=9)
+    q = climbing(c, 2.0)
+    got = c.attend(q, out=torch.zeros_like(q, dtype=out_type or q.dtype))
+    B.sdsat_paged_status(c.handle)
+    for b in (0, 2, 3):
+        for i in range(c.seqs[b][0]):
+            same = torch.equal(got[c.start[b] + i], alone(c, b, i, q, out_type=out_type))
+            assert same, f"row {i} of sequence {b}"
